@@ -308,6 +308,78 @@ PT_API pt_status pt_profile_enable(pt_ctx* ctx, int32_t on);
 PT_API pt_status pt_profile_reset(pt_ctx* ctx);
 PT_API pt_status pt_profile_read(pt_ctx* ctx, int32_t category, double* total_ms, int64_t* launches, double* work /*HOST out*/);
 
+/* ---- operators by themselves ------------------------------------------------
+ * The calls below take no context: every pointer is DEVICE memory of the
+ * caller's unless marked HOST, work is enqueued on hip_stream (of the current
+ * GPU) and nothing synchronises, allocates, or is kept from one call for the
+ * next, so they may be captured into a HIP graph.  Outputs must not overlap
+ * inputs except where that is said.  On an error nothing is enqueued
+ * (PT_EDEVICE apart); pt_last_error(NULL) has the calling thread's message. */
+
+/* Attention under a rule:
+ *   t_ij = scale q_i . k_j,  s_ij = cap tanh(t_ij / cap) - slope_h |q0 + i - j|,
+ *   o_i  = sum_j softmax_j(s_ij) v_j  over the keys j that query i sees.
+ * A query sees key j if its order allows it (PT_ATTN_FULL every key;
+ * PT_ATTN_CAUSAL j <= q0 + i; PT_ATTN_PREFIX that, or j < prefix[sample]) and
+ * both are of the same document: documents are ids >= 0 in any order; a
+ * negative id marks padding, which sees nothing and which nothing sees.  The
+ * rows of q, k, v and d_o that belong to padding are never used, whatever they
+ * hold (NaN too); a NaN or an infinity elsewhere may also reach queries of other
+ * documents in the same rows of 64.  A query that sees no key has o = 0,
+ * lse = -infinity and no gradient; so have padding rows, which are written as
+ * zeros.  Head h reads key and value head h / (H / Hkv), whose gradients are
+ * the sums over the heads that share it.  Slopes, documents and prefix lengths
+ * have no gradient.
+ *   Views: element (sample, row, head, d) is at data[sample * .sample + row *
+ * .row + head * .head + d]; data 16-byte aligned, strides multiples of 16 bytes
+ * (0 for a broadcast input).
+ *   dtype PT_BF16: products of bf16 on the matrix cores, everything else fp32,
+ * the probabilities and dS rounded to bf16 for the second products.  PT_F32: all
+ * in fp32.  Sums are in a fixed order: results do not vary from run to run. */
+enum { PT_ATTN_FULL = 0, PT_ATTN_CAUSAL = 1, PT_ATTN_PREFIX = 2 };
+typedef struct {
+  void* data;
+  int64_t sample, row, head;   /* strides in elements */
+} pt_heads;
+typedef struct {
+  int32_t dtype;            /* PT_F32 | PT_BF16, of q, k, v, o and their gradients         */
+  int32_t nb, Sq, Sk;       /* samples, queries and keys of each; 0 is allowed, Sq and Sk <= 2^18 */
+  int32_t H, Hkv, dh;       /* H % Hkv == 0; dh % 8 == 0, dh <= 128                        */
+  int32_t order;            /* PT_ATTN_*                                                   */
+  int32_t q0;               /* position of query 0 among the keys, q0 + Sq <= 2^24         */
+  float scale;              /* > 0, commonly 1 / sqrt(dh)                                  */
+  float cap;                /* 0: none                                                     */
+  const float* slopes;      /* [H] or NULL                                                 */
+  const int32_t* q_documents;   /* [nb,Sq], or NULL (then k_documents too)                 */
+  const int32_t* k_documents;   /* [nb,Sk]                                                 */
+  const int32_t* prefix;    /* [nb], PT_ATTN_PREFIX only                                   */
+} pt_attention;
+/* Bytes of scratch of pt_attention_bwd (HOST out); its contents mean nothing before and after a call.  Calls that
+ * may overlap (on two streams, or replays of two graphs) need a workspace each. */
+PT_API pt_status pt_attention_workspace(const pt_attention* a /*HOST*/, size_t* bwd_bytes);
+/* lse [nb,H,Sq]: log of the row's sum of exp(s), which the backward pass reads; may be NULL. */
+PT_API pt_status pt_attention_fwd(const pt_attention* a /*HOST*/, const pt_heads* q, const pt_heads* k, const pt_heads* v,
+                                  const pt_heads* o /*HOST structs*/, float* lse, void* hip_stream);
+/* Gradients of q, k and v, overwritten; o and lse as the forward call wrote them, under the same description. */
+PT_API pt_status pt_attention_bwd(const pt_attention* a /*HOST*/, const pt_heads* q, const pt_heads* k, const pt_heads* v,
+                                  const pt_heads* o, const float* lse, const pt_heads* d_o, const pt_heads* dq, const pt_heads* dk,
+                                  const pt_heads* dv /*HOST structs*/, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* GELU (erf form) whose input is kept in 8 bits for the backward pass: a quarter of the bytes of input and
+ * output in bf16.  A row's checkpoint is F codes and (F + 31) / 32 exponents, one for each 32 columns:
+ * x = code 2^(exponent - 127), the exponent the least with which the block's largest |h| is at most 127 steps
+ * (at least 1), codes rounded to nearest even; 255: the block held a NaN or an infinity, and is NaN.
+ *   pt_gelu8_fwd   g = GELU(h) (of h itself) and the checkpoint of h
+ *   pt_gelu8_bwd   dh = dg GELU'(x), and g = GELU(x) unless NULL (what the weight gradient behind it reads).
+ *                  dh may be dg.
+ * h, g, dg, dh [rows,F] of dtype, codes [rows,F], exps [rows,(F+31)/32], all contiguous and (but exps) 16-byte
+ * aligned; F % 4 == 0. */
+PT_API pt_status pt_gelu8_fwd(int32_t dtype, const void* h, void* g, int8_t* codes, uint8_t* exps, int64_t rows, int32_t F,
+                              void* hip_stream);
+PT_API pt_status pt_gelu8_bwd(int32_t dtype, const int8_t* codes, const uint8_t* exps, const void* dg, void* dh, void* g, int64_t rows,
+                              int32_t F, void* hip_stream);
+
+/* The message of the context's last error; with ctx NULL, of the calling thread's last error in a call that takes no context. */
 PT_API const char* pt_last_error(const pt_ctx* ctx);
 
 #ifdef __cplusplus

@@ -19,6 +19,7 @@ PT_VIT_PRELN, PT_BERT_POSTLN = 0, 1
 PT_F32, PT_BF16 = 0, 1
 PT_SGDM, PT_ADAMW = 0, 1
 PT_HEAD_DEFAULT, PT_HEAD_CLS = 0, 1
+ATTN_ORDERS = {"full": 0, "causal": 1, "prefix": 2}
 KIND_PARAM, KIND_GRAD, KIND_MOMENT1, KIND_MOMENT2, KIND_SHADOW = range(5)
 ACT_HK, ACT_HL, ACT_LOGITS, ACT_DHK = range(4)
 PROF_CATEGORIES = ("gemm_generic", "gemm_nn", "gemm_nt", "gemm_tn", "attn_fwd", "attn_bwd", "ln_fwd", "ln_bwd",
@@ -37,6 +38,16 @@ class PtConfig(C.Structure):
 class PtOptHparams(C.Structure):
     _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float),
                 ("eps", C.c_float), ("weight_decay", C.c_float)]
+
+
+class PtHeads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("sample", C.c_int64), ("row", C.c_int64), ("head", C.c_int64)]
+
+
+class PtAttention(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("nb", C.c_int32), ("Sq", C.c_int32), ("Sk", C.c_int32), ("H", C.c_int32), ("Hkv", C.c_int32),
+                ("dh", C.c_int32), ("order", C.c_int32), ("q0", C.c_int32), ("scale", C.c_float), ("cap", C.c_float),
+                ("slopes", C.c_void_p), ("q_documents", C.c_void_p), ("k_documents", C.c_void_p), ("prefix", C.c_void_p)]
 
 
 class PtError(RuntimeError):
@@ -88,6 +99,12 @@ def load_library():
         "pt_attach_host_tier": [vp, vp, sz],
         "pt_cache_prefetch": [vp, P(i64), i32, P(i32)],
         "pt_host_tier_stats": [vp, P(i64), P(i64), P(i64), P(i64)],
+        "pt_attention_workspace": [P(PtAttention), P(sz)],
+        "pt_attention_fwd": [P(PtAttention), P(PtHeads), P(PtHeads), P(PtHeads), P(PtHeads), vp, vp],
+        "pt_attention_bwd": [P(PtAttention), P(PtHeads), P(PtHeads), P(PtHeads), P(PtHeads), vp, P(PtHeads), P(PtHeads), P(PtHeads),
+                             P(PtHeads), vp, sz, vp],
+        "pt_gelu8_fwd": [i32, vp, vp, vp, vp, i64, i32, vp],
+        "pt_gelu8_bwd": [i32, vp, vp, vp, vp, vp, i64, i32, vp],
         "pt_profile_enable": [vp, i32],
         "pt_profile_reset": [vp],
         "pt_profile_read": [vp, i32, P(C.c_double), P(i64), P(C.c_double)],
@@ -132,6 +149,178 @@ def next_boundary(norms, L: int, k_prev: int, alpha: float) -> int:
     if st != PT_OK:
         raise PtError(st, "pt_next_boundary")
     return out.value
+
+
+# ---- operators by themselves (no context) ---------------------------------------
+# Tensors are PyTorch's, on one GPU; work goes to that GPU's current stream, outputs and scratch come from the caching
+# allocator on it.
+
+def _check(ok: bool, what: str):
+    if not ok:
+        raise PtError(PT_EINVAL, what)
+
+
+def _op_chk(lib, st):
+    if st != PT_OK:
+        raise PtError(st, (lib.pt_last_error(None) or b"").decode())
+
+
+def _dtype_of(t) -> int:
+    name = str(t.dtype)
+    _check(name in ("torch.float32", "torch.bfloat16"), f"dtype {name}: float32 or bfloat16")
+    return PT_BF16 if name == "torch.bfloat16" else PT_F32
+
+
+class _On:
+    """The tensors' GPU as the current one, and its current stream's handle."""
+
+    def __init__(self, *tensors):
+        import torch
+        dev = tensors[0].device
+        _check(dev.type == "cuda", f"tensors must be on a GPU, not on {dev}")
+        for t in tensors:
+            _check(t is None or t.device == dev, "tensors on several devices")
+        self.guard = None if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+        self.dev = dev
+
+    def __enter__(self):
+        import torch
+        if self.guard:
+            self.guard.__enter__()
+        return torch.cuda.current_stream(self.dev).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard:
+            self.guard.__exit__(*exc)
+
+
+def _heads(t, name: str, shape=None, dtype=None) -> PtHeads:
+    _check(t.dim() == 4, f"{name}: [samples, rows, heads, head size]")
+    _check(shape is None or tuple(t.shape) == tuple(shape), f"{name}: shape {tuple(t.shape)}, not {shape}")
+    _check(dtype is None or t.dtype == dtype, f"{name}: dtype {t.dtype}, not {dtype}")
+    a, b, c, d = t.stride()
+    _check(d == 1 or t.numel() == 0, f"{name}: the head size must be contiguous")
+    return PtHeads(t.data_ptr(), a, b, c)
+
+
+class AttentionRule:
+    """What a query sees and how its scores are bent (pt_attention in include/pt.h).
+
+    order        "full", "causal", or "prefix" (causal, and the first prefix[sample] keys)
+    scale        None: 1 / sqrt(head size)
+    cap          0, or c of c tanh(s / c)
+    slopes       float32 [H]: a bias of -slope |i - j|
+    documents    int32 [nb, keys], below 0: padding; q_documents int32 [nb, queries], None: the same tensor
+    prefix       int32 [nb]
+    q0           position of query 0 among the keys
+    """
+
+    def __init__(self, order="full", scale=None, cap=0.0, slopes=None, documents=None, q_documents=None, prefix=None, q0=0):
+        _check(order in ATTN_ORDERS, f"order {order!r}: one of {', '.join(ATTN_ORDERS)}")
+        self.order, self.scale, self.cap, self.q0 = order, scale, cap, q0
+        self.slopes, self.documents, self.prefix = slopes, documents, prefix
+        self.q_documents = documents if q_documents is None else q_documents
+        for t, kind in ((slopes, "float32"), (documents, "int32"), (self.q_documents, "int32"), (prefix, "int32")):
+            _check(t is None or (str(t.dtype) == "torch." + kind and t.is_contiguous()), f"slopes are float32, documents and prefix int32, all contiguous (got {None if t is None else t.dtype})")
+
+    def describe(self, q, k) -> PtAttention:
+        nb, Sq, H, dh = q.shape
+        Sk, Hkv = k.shape[1], k.shape[2]
+        a = PtAttention(_dtype_of(q), nb, Sq, Sk, H, Hkv, dh, ATTN_ORDERS[self.order], self.q0,
+                        (1.0 / dh ** 0.5 if dh else 1.0) if self.scale is None else self.scale, self.cap)
+        if self.slopes is not None:
+            _check(tuple(self.slopes.shape) == (H,), f"slopes: [{H}]")
+            a.slopes = self.slopes.data_ptr()
+        if self.q_documents is not None:
+            _check(self.documents is not None, "documents of the queries and of the keys go together")
+            _check(tuple(self.documents.shape) == (nb, Sk), f"documents: [{nb}, {Sk}]")
+            _check(tuple(self.q_documents.shape) == (nb, Sq), f"q_documents: [{nb}, {Sq}]")
+            a.q_documents, a.k_documents = self.q_documents.data_ptr(), self.documents.data_ptr()
+        if self.order == "prefix":
+            _check(self.prefix is not None and tuple(self.prefix.shape) == (nb,), f"prefix: [{nb}]")
+            a.prefix = self.prefix.data_ptr()
+        return a
+
+    def tensors(self):
+        return self.slopes, self.documents, self.q_documents, self.prefix
+
+
+def attention_forward(q, k, v, rule: AttentionRule | None = None, out=None, want_lse: bool = True):
+    """(o, lse): q [nb, Sq, H, dh], k and v [nb, Sk, Hkv, dh], views of any strides that are multiples of 16 bytes; o like q, lse
+    float32 [nb, H, Sq] (None if not wanted)."""
+    import torch
+    rule = rule or AttentionRule()
+    hq = _heads(q, "q")
+    nb, Sq, H, dh = q.shape
+    hk = _heads(k, "k", (nb, *k.shape[1:3], dh), q.dtype)
+    hv = _heads(v, "v", k.shape, q.dtype)
+    a = rule.describe(q, k)
+    with _On(q, k, v, out, *rule.tensors()) as stream:
+        o = torch.empty(nb, Sq, H, dh, dtype=q.dtype, device=q.device) if out is None else out
+        ho = _heads(o, "out", q.shape, q.dtype)
+        lse = torch.empty(nb, H, Sq, dtype=torch.float32, device=q.device) if want_lse else None
+        lib = load_library()
+        _op_chk(lib, lib.pt_attention_fwd(a, hq, hk, hv, ho, lse.data_ptr() if want_lse else None, stream))
+    return o, lse
+
+
+def attention_backward(q, k, v, o, lse, do, rule: AttentionRule | None = None, grads=None):
+    """(dq, dk, dv) of the call that returned (o, lse); grads: tensors (views) to write them to."""
+    import torch
+    rule = rule or AttentionRule()
+    hq = _heads(q, "q")
+    nb, Sq, H, dh = q.shape
+    hk = _heads(k, "k", (nb, *k.shape[1:3], dh), q.dtype)
+    hv, ho, hd = _heads(v, "v", k.shape, q.dtype), _heads(o, "o", q.shape, q.dtype), _heads(do, "do", q.shape, q.dtype)
+    _check(lse is not None and str(lse.dtype) == "torch.float32" and tuple(lse.shape) == (nb, H, Sq) and lse.is_contiguous(),
+           f"lse: float32 [{nb}, {H}, {Sq}], contiguous")
+    a = rule.describe(q, k)
+    with _On(q, k, v, o, lse, do, *(grads or ()), *rule.tensors()) as stream:
+        dq, dk, dv = grads or (torch.empty(nb, Sq, H, dh, dtype=q.dtype, device=q.device),
+                               *(torch.empty(*k.shape, dtype=q.dtype, device=q.device) for _ in range(2)))
+        g = _heads(dq, "dq", q.shape, q.dtype), _heads(dk, "dk", k.shape, q.dtype), _heads(dv, "dv", k.shape, q.dtype)
+        lib, need = load_library(), C.c_size_t()
+        _op_chk(lib, lib.pt_attention_workspace(a, need))
+        ws = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+        _op_chk(lib, lib.pt_attention_bwd(a, hq, hk, hv, ho, lse.data_ptr(), hd, *g, ws.data_ptr(), need.value, stream))
+    return dq, dk, dv
+
+
+def _rows(t, name: str):
+    _check(t.dim() == 2 and t.is_contiguous(), f"{name}: [rows, F], contiguous")
+
+
+def gelu8_forward(h):
+    """(g, codes, exps): GELU of h [rows, F] and the 8-bit checkpoint of h that gelu8_backward reads."""
+    import torch
+    _rows(h, "h")
+    T, F = h.shape
+    with _On(h) as stream:
+        g = torch.empty_like(h)
+        codes = torch.empty(T, F, dtype=torch.int8, device=h.device)
+        exps = torch.empty(T, (F + 31) // 32, dtype=torch.uint8, device=h.device)
+        lib = load_library()
+        _op_chk(lib, lib.pt_gelu8_fwd(_dtype_of(h), h.data_ptr(), g.data_ptr(), codes.data_ptr(), exps.data_ptr(), T, F, stream))
+    return g, codes, exps
+
+
+def gelu8_backward(codes, exps, dg, want_activation: bool = True, out=None):
+    """(dh, g): dg GELU'(x) and GELU(x) (None if not wanted) of the checkpointed x; out: where dh goes (it may be dg itself)."""
+    import torch
+    _rows(dg, "dg")
+    T, F = dg.shape
+    _check(str(codes.dtype) == "torch.int8" and tuple(codes.shape) == (T, F) and codes.is_contiguous(), f"codes: int8 [{T}, {F}]")
+    _check(str(exps.dtype) == "torch.uint8" and tuple(exps.shape) == (T, (F + 31) // 32) and exps.is_contiguous(),
+           f"exps: uint8 [{T}, {(F + 31) // 32}]")
+    with _On(dg, codes, exps, out) as stream:
+        dh = torch.empty_like(dg) if out is None else out
+        _rows(dh, "out")
+        _check(dh.shape == dg.shape and dh.dtype == dg.dtype, f"out: {dg.dtype} [{T}, {F}]")
+        g = torch.empty_like(dg) if want_activation else None
+        lib = load_library()
+        _op_chk(lib, lib.pt_gelu8_bwd(_dtype_of(dg), codes.data_ptr(), exps.data_ptr(), dg.data_ptr(), dh.data_ptr(),
+                                      g.data_ptr() if want_activation else None, T, F, stream))
+    return dh, g
 
 
 class Context:

@@ -1,0 +1,308 @@
+// Attention under a rule in fp32 on the fp32 matrix instructions (the formulas, the masks and the list of tiles are those of
+// attention_rules.hip; the tiles and fragments those of attention_f32_tile.h), and delta_i = dO_i . o_i for both types.
+//
+// A wave owns 16 rows, a workgroup 64; the other side streams through LDS in tiles of 64 rows.  Bound by the fp32 matrix rate.
+#include "attention_rules.h"
+#include "attention_f32_tile.h"
+
+namespace pt {
+namespace {
+
+// scores in the log2 domain, with the library's tanh (scores are held to fp32's rounding here)
+struct ScoreF {
+  float c, scale, cap, inv_cap, a, sl;
+  __device__ __forceinline__ ScoreF(const AttnRuleArgs& g, int h) {
+    constexpr float kLog2e = 1.44269504088896f;
+    scale = g.scale;
+    c = g.scale * kLog2e;
+    cap = g.cap;
+    inv_cap = g.cap > 0.f ? g.scale / g.cap : 0.f;
+    a = g.cap * kLog2e;
+    sl = g.slopes ? -g.slopes[h] * kLog2e : 0.f;
+  }
+  // *bent: tanh, 0 without a cap
+  __device__ __forceinline__ float at(float s, float dist, float* bent) const {
+    *bent = cap > 0.f ? tanhf(s * inv_cap) : 0.f;
+    const float x = cap > 0.f ? a * *bent : s * c;
+    return fmaf(sl, dist, x);
+  }
+};
+
+// a staged tile; padding rows (which may hold anything) become zeros
+template <typename A>
+__device__ __forceinline__ void rule_store(float* s, int tid, const f32x4 (&reg)[A::N4], const int* docs) {
+#pragma unroll
+  for (int i = 0; i < A::N4; ++i) {
+    int row, d;
+    A::place(tid, i, &row, &d);
+    *reinterpret_cast<f32x4*>(s + row * A::LD + d) = docs[row] >= 0 ? reg[i] : f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+}
+
+template <int DP>
+__global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_fwd_f32_kernel(AttnRuleArgs g) {
+  typedef AttnTile<float, DP> A;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  float* xs = reinterpret_cast<float*>(smem);
+  float* ys = xs + A::FLOATS;
+  int* kdoc = reinterpret_cast<int*>(ys + A::FLOATS);
+  RuleList list(kdoc + kRuleTile);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, gr = lane >> 4, l = lane & 15;
+  const RuleUnit u(g, (g.Sq + 63) / 64, g.H);
+  const int b = u.b, h = u.h, hk = h / (g.H / g.Hkv);
+  const int i = u.blk * 64 + wave * 16 + l;
+  const RuleRows rows(g, b);
+  const int lim = rows.lim(g, i), qd = rows.qdoc(g, i);
+  const bool ok = i < g.Sq, on = ok && qd >= 0;
+  const int n = list.keys(g, rows, wave, lane, ok, lim, qd);
+  const float* kp = static_cast<const float*>(g.k.p) + b * g.k.b + hk * g.k.h;
+  const float* vp = static_cast<const float*>(g.v.p) + b * g.v.b + hk * g.v.h;
+  const ScoreF sc(g, h);
+  f32x4 q[A::NF], o[A::NF], rk[A::N4], rv[A::N4];
+  A::own(static_cast<const float*>(g.q.p) + b * g.q.b + h * g.q.h, g.q.t, on ? i : g.Sq, g.Sq, g.dh, gr, 1.f, q);
+#pragma unroll
+  for (int x = 0; x < A::NF; ++x) o[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -1e30f, sum = 0.f;
+  int rd = 0;
+  auto load = [&](int it) {
+    const int j0 = list.tile(it) * kRuleTile;
+    A::load(kp, g.k.t, j0, g.Sk, g.dh, tid, rk);
+    A::load(vp, g.v.t, j0, g.Sk, g.dh, tid, rv);
+    if (tid < kRuleTile) rd = rows.kdoc(g, j0 + tid);
+  };
+  if (n > 0) load(0);
+  for (int it = 0; it < n; ++it) {
+    __syncthreads();
+    if (tid < kRuleTile) kdoc[tid] = rd;
+    __syncthreads();
+    rule_store<A>(xs, tid, rk, kdoc);
+    rule_store<A>(ys, tid, rv, kdoc);
+    __syncthreads();
+    if (it + 1 < n) load(it + 1);
+    if (!list.needed(it, wave)) continue;
+    const int j0 = list.tile(it) * kRuleTile;
+    const float at = (float)(g.q0 + i - j0);
+    f32x4 s[4];
+    float mx = m;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      s[x] = A::dot(xs, 16 * x, l, gr, q);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int r = 16 * x + 4 * gr + v;
+        float bent;
+        s[x][v] = sc.at(s[x][v], fabsf(at - (float)r), &bent);
+        if (kdoc[r] != qd || j0 + r > lim) s[x][v] = -INFINITY;
+        mx = fmaxf(mx, s[x][v]);
+      }
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float alpha = __builtin_amdgcn_exp2f(m - mx);
+    m = mx;
+    sum *= alpha;
+#pragma unroll
+    for (int x = 0; x < A::NF; ++x) o[x] *= alpha;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        s[x][v] = __builtin_amdgcn_exp2f(s[x][v] - mx);
+        sum += s[x][v];
+      }
+      A::add(ys, 16 * x, l, gr, s[x], o);
+    }
+  }
+  sum += __shfl_xor(sum, 16, 64);
+  sum += __shfl_xor(sum, 32, 64);
+  if (!ok) return;
+  A::put(static_cast<float*>(const_cast<void*>(g.o.p)) + b * g.o.b + (int64_t)i * g.o.t + h * g.o.h, g.dh, gr, sum > 0.f ? 1.f / sum : 0.f, o);
+  if (g.lse && gr == 0) g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i] = sum > 0.f ? (m + log2f(sum)) * 0.693147180559945f : -INFINITY;
+}
+
+// a probability this near 1 means a query that sees one key: dS is exactly 0 then (see attention_rules.hip)
+constexpr float kOneKeyF = 1.f - 1.f / 262144.f;
+
+template <int DP>
+__global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(AttnRuleArgs g, int ndkv) {
+  typedef AttnTile<float, DP> A;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  float* xs = reinterpret_cast<float*>(smem);
+  float* ys = xs + A::FLOATS;
+  float* ls = ys + A::FLOATS;                            // [lse][delta]
+  int* docs = reinterpret_cast<int*>(ls + 2 * kRuleTile);   // [document][lim]
+  RuleList list(docs + 2 * kRuleTile);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, gr = lane >> 4, l = lane & 15;
+  f32x4 rx[A::N4], ry[A::N4], a0[A::NF], a1[A::NF], ax[A::NF];
+#pragma unroll
+  for (int x = 0; x < A::NF; ++x) ax[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if ((int)blockIdx.x >= ndkv) {   // dq of 64 queries
+    const RuleUnit u(g, (g.Sq + 63) / 64, g.H, blockIdx.x - ndkv);
+    const int b = u.b, h = u.h, hk = h / (g.H / g.Hkv);
+    const int i = u.blk * 64 + wave * 16 + l;
+    const RuleRows rows(g, b);
+    const int lim = rows.lim(g, i), qd = rows.qdoc(g, i);
+    const bool ok = i < g.Sq, on = ok && qd >= 0;
+    const int n = list.keys(g, rows, wave, lane, ok, lim, qd);
+    A::own(static_cast<const float*>(g.q.p) + b * g.q.b + h * g.q.h, g.q.t, on ? i : g.Sq, g.Sq, g.dh, gr, 1.f, a0);
+    A::own(static_cast<const float*>(g.d_o.p) + b * g.d_o.b + h * g.d_o.h, g.d_o.t, on ? i : g.Sq, g.Sq, g.dh, gr, 1.f, a1);
+    const float* kp = static_cast<const float*>(g.k.p) + b * g.k.b + hk * g.k.h;
+    const float* vp = static_cast<const float*>(g.v.p) + b * g.v.b + hk * g.v.h;
+    const ScoreF sc(g, h);
+    const float lw = on ? rule_lse2(g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i]) : INFINITY;
+    const float dl = on ? g.delta[((int64_t)b * g.H + h) * g.Sq + i] : 0.f;
+    int rd = 0;
+    auto load = [&](int it) {
+      const int j0 = list.tile(it) * kRuleTile;
+      A::load(kp, g.k.t, j0, g.Sk, g.dh, tid, rx);
+      A::load(vp, g.v.t, j0, g.Sk, g.dh, tid, ry);
+      if (tid < kRuleTile) rd = rows.kdoc(g, j0 + tid);
+    };
+    if (n > 0) load(0);
+    for (int it = 0; it < n; ++it) {
+      __syncthreads();
+      if (tid < kRuleTile) docs[tid] = rd;
+      __syncthreads();
+      rule_store<A>(xs, tid, rx, docs);
+      rule_store<A>(ys, tid, ry, docs);
+      __syncthreads();
+      if (it + 1 < n) load(it + 1);
+      if (!list.needed(it, wave)) continue;
+      const int j0 = list.tile(it) * kRuleTile;
+      const float at = (float)(g.q0 + i - j0);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        f32x4 s = A::dot(xs, 16 * x, l, gr, a0);
+        const f32x4 dp = A::dot(ys, 16 * x, l, gr, a1);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const int r = 16 * x + 4 * gr + v;
+          float bent;
+          const float p = __builtin_amdgcn_exp2f(sc.at(s[v], fabsf(at - (float)r), &bent) - lw);
+          const bool see = docs[r] == qd && j0 + r <= lim && p < kOneKeyF;
+          s[v] = see ? p * (dp[v] - dl) * (1.f - bent * bent) : 0.f;
+        }
+        A::add(xs, 16 * x, l, gr, s, ax);
+      }
+    }
+    if (ok) A::put(static_cast<float*>(const_cast<void*>(g.dq.p)) + b * g.dq.b + (int64_t)i * g.dq.t + h * g.dq.h, g.dh, gr, g.scale, ax);
+    return;
+  }
+  // dk and dv of 64 keys
+  const int G = g.H / g.Hkv;
+  const RuleUnit u(g, (g.Sk + 63) / 64, g.Hkv, blockIdx.x);
+  const int b = u.b, hk = u.h;
+  const int j = u.blk * 64 + wave * 16 + l;
+  const RuleRows rows(g, b);
+  const int kd = rows.kdoc(g, j);
+  const bool ok = j < g.Sk, on = ok && kd >= 0;
+  const int n = list.queries(g, rows, wave, lane, ok, j, kd);
+  A::own(static_cast<const float*>(g.k.p) + b * g.k.b + hk * g.k.h, g.k.t, on ? j : g.Sk, g.Sk, g.dh, gr, 1.f, a0);
+  A::own(static_cast<const float*>(g.v.p) + b * g.v.b + hk * g.v.h, g.v.t, on ? j : g.Sk, g.Sk, g.dh, gr, 1.f, a1);
+  f32x4 ay[A::NF];
+#pragma unroll
+  for (int x = 0; x < A::NF; ++x) ay[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+  int rd = 0, rlim = 0;
+  float rl = 0.f, rdl = 0.f;
+  auto load = [&](int it) {
+    const int h = hk * G + it / n, i0 = list.tile(it % n) * kRuleTile;
+    A::load(static_cast<const float*>(g.q.p) + b * g.q.b + h * g.q.h, g.q.t, i0, g.Sq, g.dh, tid, rx);
+    A::load(static_cast<const float*>(g.d_o.p) + b * g.d_o.b + h * g.d_o.h, g.d_o.t, i0, g.Sq, g.dh, tid, ry);
+    if (tid < kRuleTile) {
+      const int i = i0 + tid;
+      rd = rows.qdoc(g, i);
+      rlim = rows.lim(g, i);
+      rl = i < g.Sq && rd >= 0 ? rule_lse2(g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i]) : INFINITY;
+      rdl = i < g.Sq ? g.delta[((int64_t)b * g.H + h) * g.Sq + i] : 0.f;
+    }
+  };
+  const int total = n * G;
+  if (total > 0) load(0);
+  for (int it = 0; it < total; ++it) {
+    __syncthreads();
+    if (tid < kRuleTile) { docs[tid] = rd; docs[kRuleTile + tid] = rlim; ls[tid] = rl; ls[kRuleTile + tid] = rdl; }
+    __syncthreads();
+    rule_store<A>(xs, tid, rx, docs);
+    rule_store<A>(ys, tid, ry, docs);
+    __syncthreads();
+    if (it + 1 < total) load(it + 1);
+    const int item = it % n;
+    if (!list.needed(item, wave)) continue;
+    const ScoreF sc(g, hk * G + it / n);
+    const float at = (float)(g.q0 + list.tile(item) * kRuleTile - j);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      f32x4 p = A::dot(xs, 16 * x, l, gr, a0);
+      f32x4 ds = A::dot(ys, 16 * x, l, gr, a1);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int r = 16 * x + 4 * gr + v;
+        float bent;
+        const float e = __builtin_amdgcn_exp2f(sc.at(p[v], fabsf(at + (float)r), &bent) - ls[r]);
+        const bool see = docs[r] == kd && j <= docs[kRuleTile + r];
+        p[v] = see ? e : 0.f;
+        ds[v] = see && e < kOneKeyF ? e * (ds[v] - ls[kRuleTile + r]) * (1.f - bent * bent) : 0.f;
+      }
+      A::add(ys, 16 * x, l, gr, p, ay);
+      A::add(xs, 16 * x, l, gr, ds, ax);
+    }
+  }
+  if (ok) {
+    A::put(static_cast<float*>(const_cast<void*>(g.dk.p)) + b * g.dk.b + (int64_t)j * g.dk.t + hk * g.dk.h, g.dh, gr, g.scale, ax);
+    A::put(static_cast<float*>(const_cast<void*>(g.dv.p)) + b * g.dv.b + (int64_t)j * g.dv.t + hk * g.dv.h, g.dh, gr, 1.f, ay);
+  }
+}
+
+// delta[b, h, i] = dO . o of one query and head, 0 for padding (whose rows may hold anything).  16 lanes a row; rows are taken
+// with the heads next to each other, as a packed layout has them.
+template <typename T>
+__global__ __launch_bounds__(256) void rule_delta_kernel(AttnRuleArgs g) {
+  const int64_t r = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), total = (int64_t)g.nb * g.Sq * g.H;
+  if (r >= total) return;
+  const int h = (int)(r % g.H), l = threadIdx.x & 15;
+  const int64_t t = r / g.H;
+  const int i = (int)(t % g.Sq), b = (int)(t / g.Sq);
+  const RuleRows rows(g, b);
+  const T* o = static_cast<const T*>(g.o.p) + b * g.o.b + (int64_t)i * g.o.t + h * g.o.h;
+  const T* d = static_cast<const T*>(g.d_o.p) + b * g.d_o.b + (int64_t)i * g.d_o.t + h * g.d_o.h;
+  float s = 0.f;
+  for (int c = 4 * l; c < g.dh; c += 64) {
+    const f32x4 a = load4(o + c), e = load4(d + c);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) s = fmaf(a[x], e[x], s);
+  }
+#pragma unroll
+  for (int x = 1; x < 16; x <<= 1) s += __shfl_xor(s, x, 64);
+  if (l == 0) g.delta[((int64_t)b * g.H + h) * g.Sq + i] = rows.qdoc(g, i) >= 0 ? s : 0.f;
+}
+
+template <int DP>
+hipError_t launch_f32(const AttnRuleArgs& g, bool bwd, hipStream_t st) {
+  const int nt = ((bwd && g.Sq > g.Sk ? g.Sq : g.Sk) + kRuleTile - 1) / kRuleTile;
+  const size_t lds = (size_t)2 * AttnTile<float, DP>::FLOATS * 4 + (bwd ? 4 : 1) * kRuleTile * 4 + RuleList::ints(nt) * 4;
+  const int nq = g.nb * g.H * ((g.Sq + 63) / 64), nk = g.nb * g.Hkv * ((g.Sk + 63) / 64);
+  if ((bwd ? nk + nq : nq) == 0) return hipSuccess;
+  if (bwd) PT_RULE_LDS(rule_bwd_f32_kernel<DP>, lds);
+  else PT_RULE_LDS(rule_fwd_f32_kernel<DP>, lds);
+  if (bwd) hipLaunchKernelGGL(rule_bwd_f32_kernel<DP>, dim3(nk + nq), dim3(256), lds, st, g, nk);
+  else hipLaunchKernelGGL(rule_fwd_f32_kernel<DP>, dim3(nq), dim3(256), lds, st, g);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t attention_rule_f32(const AttnRuleArgs& g, bool bwd, hipStream_t st) {
+  if (g.dh <= 16) return launch_f32<16>(g, bwd, st);
+  if (g.dh <= 32) return launch_f32<32>(g, bwd, st);
+  if (g.dh <= 64) return launch_f32<64>(g, bwd, st);
+  return launch_f32<128>(g, bwd, st);
+}
+
+hipError_t attention_rule_delta(int dt, const AttnRuleArgs& g, hipStream_t st) {
+  const int blocks = (int)(((int64_t)g.nb * g.Sq * g.H + 15) / 16);
+  if (dt) hipLaunchKernelGGL(rule_delta_kernel<bf16>, dim3(blocks), dim3(256), 0, st, g);
+  else hipLaunchKernelGGL(rule_delta_kernel<float>, dim3(blocks), dim3(256), 0, st, g);
+  return hipGetLastError();
+}
+
+}  // namespace pt

@@ -59,6 +59,33 @@ void attention_fwd_first_query(int dt, const void* qkv, void* ctx_rows, float* l
 void attention_bwd_first_query(int dt, const void* qkv, const void* ctx_rows, const void* do_rows, const float* lse,
                                void* dqkv, int nb, int S, int H, int dh, hipStream_t st);
 
+// ---- attention under a rule (formulas: attention_rules.hip) over strided views [nb, rows, heads, dh], dh contiguous
+struct HeadView { const void* p; int64_t b, t, h; };   // strides in elements: sample, row, head
+struct AttnRuleArgs {
+  int nb, Sq, Sk, H, Hkv, dh;
+  int order;                 // 0 every key, 1 causal, 2 causal behind a prefix
+  int q0;                    // position of query 0 among the keys
+  float scale, cap;          // cap 0: none
+  const float* slopes;       // [H] or null
+  const int32_t* qdoc;       // [*, Sq] or null; below 0: padding
+  const int32_t* kdoc;       // [*, Sk] or null
+  const int32_t* prefix;     // [*], order 2
+  const int64_t* bmap;       // sample b's documents and prefix are those of row bmap[b]; null: b
+  HeadView q, k, v, o, d_o, dq, dk, dv;
+  float* lse; int64_t lse_b, lse_h;   // forward: written unless null; backward: read
+  float* delta;              // backward: scratch [nb, H, Sq]
+};
+constexpr int kRuleMaxRows = 1 << 18;   // of queries or keys: the list of tiles lives in LDS
+hipError_t attention_rule_fwd(int dt, const AttnRuleArgs& g, hipStream_t st);
+hipError_t attention_rule_bwd(int dt, const AttnRuleArgs& g, hipStream_t st);
+hipError_t attention_rule_bf16(const AttnRuleArgs& g, bool bwd, hipStream_t st);
+hipError_t attention_rule_f32(const AttnRuleArgs& g, bool bwd, hipStream_t st);
+hipError_t attention_rule_delta(int dt, const AttnRuleArgs& g, hipStream_t st);
+
+// ---- GELU with an 8-bit checkpoint of its input (format: gelu8.hip); rows of F % 4 == 0 values; dh may be dg, g may be null
+hipError_t gelu8_fwd(int dt, const void* h, void* g, int8_t* codes, uint8_t* exps, int64_t rows, int F, hipStream_t st);
+hipError_t gelu8_bwd(int dt, const int8_t* codes, const uint8_t* exps, const void* dg, void* dh, void* g, int64_t rows, int F, hipStream_t st);
+
 // ---- LayerNorm over rows of length D
 // y[r] = LN(x[r]); rows addressed r*ldx / r*ldy (elements).  x is fp32 when x_f32, else T.
 // mean/rstd may be null.

@@ -18,6 +18,7 @@
 
 #include "kernels.h"
 #include "gemm_rules.h"
+#include "ops.h"
 
 using namespace pt;
 
@@ -942,7 +943,7 @@ pt_status pt_destroy(pt_ctx* c) {
   return PT_OK;
 }
 
-const char* pt_last_error(const pt_ctx* c) { return c ? c->err.c_str() : "null context"; }
+const char* pt_last_error(const pt_ctx* c) { return c ? c->err.c_str() : ops_last_error(); }
 
 pt_status pt_get_freeze_boundary(const pt_ctx* c, int32_t* k) {
   if (!c || !k) return PT_EINVAL;
