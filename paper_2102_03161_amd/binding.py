@@ -153,11 +153,22 @@ def next_boundary(norms, L: int, k_prev: int, alpha: float) -> int:
 
 # ---- operators by themselves (no context) ---------------------------------------
 # Tensors are PyTorch's, on one GPU; work goes to that GPU's current stream, outputs and scratch come from the caching
-# allocator on it.
+# allocator on it.  A call takes the host about as long as a short kernel takes the GPU, so nothing here formats a message
+# or imports a module unless something is wrong.
+_torch = None
+_DTYPES = {}
 
-def _check(ok: bool, what: str):
-    if not ok:
-        raise PtError(PT_EINVAL, what)
+
+def _op_setup():
+    global _torch
+    import torch
+    _torch = torch
+    _DTYPES.update({torch.float32: PT_F32, torch.bfloat16: PT_BF16})
+    return torch
+
+
+def _refuse(what: str):
+    raise PtError(PT_EINVAL, what)
 
 
 def _op_chk(lib, st):
@@ -166,41 +177,44 @@ def _op_chk(lib, st):
 
 
 def _dtype_of(t) -> int:
-    name = str(t.dtype)
-    _check(name in ("torch.float32", "torch.bfloat16"), f"dtype {name}: float32 or bfloat16")
-    return PT_BF16 if name == "torch.bfloat16" else PT_F32
+    if not _DTYPES:
+        _op_setup()
+    d = _DTYPES.get(t.dtype)
+    return _refuse(f"dtype {t.dtype}: float32 or bfloat16") if d is None else d
 
 
-class _On:
-    """The tensors' GPU as the current one, and its current stream's handle."""
-
-    def __init__(self, *tensors):
-        import torch
-        dev = tensors[0].device
-        _check(dev.type == "cuda", f"tensors must be on a GPU, not on {dev}")
-        for t in tensors:
-            _check(t is None or t.device == dev, "tensors on several devices")
-        self.guard = None if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
-        self.dev = dev
-
-    def __enter__(self):
-        import torch
-        if self.guard:
-            self.guard.__enter__()
-        return torch.cuda.current_stream(self.dev).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard:
-            self.guard.__exit__(*exc)
+def _device_of(first, *others) -> int:
+    """The index of the GPU that all tensors are on (None: no tensor)."""
+    at = first.get_device()
+    if at < 0:
+        _refuse(f"tensors must be on a GPU, not on {first.device}")
+    for t in others:
+        if t is not None and t.get_device() != at:
+            _refuse(f"a tensor on {t.device}, the first on {first.device}")
+    return at
 
 
-def _heads(t, name: str, shape=None, dtype=None) -> PtHeads:
-    _check(t.dim() == 4, f"{name}: [samples, rows, heads, head size]")
-    _check(shape is None or tuple(t.shape) == tuple(shape), f"{name}: shape {tuple(t.shape)}, not {shape}")
-    _check(dtype is None or t.dtype == dtype, f"{name}: dtype {t.dtype}, not {dtype}")
+def _launch(at: int, call, *args):
+    """call(*args, current stream of GPU `at`), with that GPU as the current one."""
+    if at == _torch.cuda.current_device():
+        return call(*args, _torch._C._cuda_getCurrentRawStream(at))
+    with _torch.cuda.device(at):
+        return call(*args, _torch._C._cuda_getCurrentRawStream(at))
+
+
+def _heads(t, name: str, shape, dtype) -> PtHeads:
+    if t.shape != shape or t.dtype is not dtype:
+        _refuse(f"{name}: {t.dtype} {tuple(t.shape)}, not {dtype} {tuple(shape)}")
     a, b, c, d = t.stride()
-    _check(d == 1 or t.numel() == 0, f"{name}: the head size must be contiguous")
+    if d != 1 and t.numel() > 0:
+        _refuse(f"{name}: the head size must be contiguous")
     return PtHeads(t.data_ptr(), a, b, c)
+
+
+def _plain(t, dtype, shape, name: str):
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(f"{name}: {dtype} {list(shape)}, contiguous (got {t.dtype} {list(t.shape)})")
+    return t.data_ptr()
 
 
 class AttentionRule:
@@ -216,110 +230,108 @@ class AttentionRule:
     """
 
     def __init__(self, order="full", scale=None, cap=0.0, slopes=None, documents=None, q_documents=None, prefix=None, q0=0):
-        _check(order in ATTN_ORDERS, f"order {order!r}: one of {', '.join(ATTN_ORDERS)}")
+        if order not in ATTN_ORDERS:
+            _refuse(f"order {order!r}: one of {', '.join(ATTN_ORDERS)}")
         self.order, self.scale, self.cap, self.q0 = order, scale, cap, q0
         self.slopes, self.documents, self.prefix = slopes, documents, prefix
         self.q_documents = documents if q_documents is None else q_documents
-        for t, kind in ((slopes, "float32"), (documents, "int32"), (self.q_documents, "int32"), (prefix, "int32")):
-            _check(t is None or (str(t.dtype) == "torch." + kind and t.is_contiguous()), f"slopes are float32, documents and prefix int32, all contiguous (got {None if t is None else t.dtype})")
+        if self.q_documents is not None and documents is None:
+            _refuse("documents of the queries and of the keys go together")
 
     def describe(self, q, k) -> PtAttention:
+        if q.dim() != 4 or k.dim() != 4:
+            _refuse("q, k and v: [samples, rows, heads, head size]")
         nb, Sq, H, dh = q.shape
-        Sk, Hkv = k.shape[1], k.shape[2]
-        a = PtAttention(_dtype_of(q), nb, Sq, Sk, H, Hkv, dh, ATTN_ORDERS[self.order], self.q0,
-                        (1.0 / dh ** 0.5 if dh else 1.0) if self.scale is None else self.scale, self.cap)
+        Sk, Hkv = k.shape[1:3]
+        dtype = _dtype_of(q)
+        a = PtAttention(dtype, nb, Sq, Sk, H, Hkv, dh, ATTN_ORDERS[self.order], self.q0,
+                        (dh ** -0.5 if dh else 1.0) if self.scale is None else self.scale, self.cap)
         if self.slopes is not None:
-            _check(tuple(self.slopes.shape) == (H,), f"slopes: [{H}]")
-            a.slopes = self.slopes.data_ptr()
-        if self.q_documents is not None:
-            _check(self.documents is not None, "documents of the queries and of the keys go together")
-            _check(tuple(self.documents.shape) == (nb, Sk), f"documents: [{nb}, {Sk}]")
-            _check(tuple(self.q_documents.shape) == (nb, Sq), f"q_documents: [{nb}, {Sq}]")
-            a.q_documents, a.k_documents = self.q_documents.data_ptr(), self.documents.data_ptr()
+            a.slopes = _plain(self.slopes, _torch.float32, (H,), "slopes")
+        if self.documents is not None:
+            a.k_documents = _plain(self.documents, _torch.int32, (nb, Sk), "documents")
+            a.q_documents = _plain(self.q_documents, _torch.int32, (nb, Sq), "q_documents")
         if self.order == "prefix":
-            _check(self.prefix is not None and tuple(self.prefix.shape) == (nb,), f"prefix: [{nb}]")
-            a.prefix = self.prefix.data_ptr()
+            if self.prefix is None:
+                _refuse("order \"prefix\" needs prefix lengths")
+            a.prefix = _plain(self.prefix, _torch.int32, (nb,), "prefix")
         return a
 
-    def tensors(self):
-        return self.slopes, self.documents, self.q_documents, self.prefix
+
+_FULL = AttentionRule()
 
 
 def attention_forward(q, k, v, rule: AttentionRule | None = None, out=None, want_lse: bool = True):
     """(o, lse): q [nb, Sq, H, dh], k and v [nb, Sk, Hkv, dh], views of any strides that are multiples of 16 bytes; o like q, lse
     float32 [nb, H, Sq] (None if not wanted)."""
-    import torch
-    rule = rule or AttentionRule()
-    hq = _heads(q, "q")
-    nb, Sq, H, dh = q.shape
-    hk = _heads(k, "k", (nb, *k.shape[1:3], dh), q.dtype)
-    hv = _heads(v, "v", k.shape, q.dtype)
+    rule = rule or _FULL
     a = rule.describe(q, k)
-    with _On(q, k, v, out, *rule.tensors()) as stream:
-        o = torch.empty(nb, Sq, H, dh, dtype=q.dtype, device=q.device) if out is None else out
-        ho = _heads(o, "out", q.shape, q.dtype)
-        lse = torch.empty(nb, H, Sq, dtype=torch.float32, device=q.device) if want_lse else None
-        lib = load_library()
-        _op_chk(lib, lib.pt_attention_fwd(a, hq, hk, hv, ho, lse.data_ptr() if want_lse else None, stream))
+    qs, ks, dtype = q.shape, k.shape, q.dtype
+    if ks[0] != qs[0] or ks[3] != qs[3]:
+        _refuse(f"q {tuple(qs)} and k {tuple(ks)} differ in samples or head size")
+    hq, hk, hv = _heads(q, "q", qs, dtype), _heads(k, "k", ks, dtype), _heads(v, "v", ks, dtype)
+    at = _device_of(q, k, v, out, rule.slopes, rule.documents, rule.q_documents, rule.prefix)
+    o = _torch.empty(qs, dtype=dtype, device=q.device) if out is None else out
+    lse = _torch.empty((qs[0], qs[2], qs[1]), dtype=_torch.float32, device=q.device) if want_lse else None
+    lib = _lib or load_library()
+    _op_chk(lib, _launch(at, lib.pt_attention_fwd, a, hq, hk, hv, _heads(o, "out", qs, dtype), lse.data_ptr() if want_lse else None))
     return o, lse
 
 
 def attention_backward(q, k, v, o, lse, do, rule: AttentionRule | None = None, grads=None):
     """(dq, dk, dv) of the call that returned (o, lse); grads: tensors (views) to write them to."""
-    import torch
-    rule = rule or AttentionRule()
-    hq = _heads(q, "q")
-    nb, Sq, H, dh = q.shape
-    hk = _heads(k, "k", (nb, *k.shape[1:3], dh), q.dtype)
-    hv, ho, hd = _heads(v, "v", k.shape, q.dtype), _heads(o, "o", q.shape, q.dtype), _heads(do, "do", q.shape, q.dtype)
-    _check(lse is not None and str(lse.dtype) == "torch.float32" and tuple(lse.shape) == (nb, H, Sq) and lse.is_contiguous(),
-           f"lse: float32 [{nb}, {H}, {Sq}], contiguous")
+    rule = rule or _FULL
     a = rule.describe(q, k)
-    with _On(q, k, v, o, lse, do, *(grads or ()), *rule.tensors()) as stream:
-        dq, dk, dv = grads or (torch.empty(nb, Sq, H, dh, dtype=q.dtype, device=q.device),
-                               *(torch.empty(*k.shape, dtype=q.dtype, device=q.device) for _ in range(2)))
-        g = _heads(dq, "dq", q.shape, q.dtype), _heads(dk, "dk", k.shape, q.dtype), _heads(dv, "dv", k.shape, q.dtype)
-        lib, need = load_library(), C.c_size_t()
-        _op_chk(lib, lib.pt_attention_workspace(a, need))
-        ws = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-        _op_chk(lib, lib.pt_attention_bwd(a, hq, hk, hv, ho, lse.data_ptr(), hd, *g, ws.data_ptr(), need.value, stream))
+    qs, ks, dtype = q.shape, k.shape, q.dtype
+    if ks[0] != qs[0] or ks[3] != qs[3]:
+        _refuse(f"q {tuple(qs)} and k {tuple(ks)} differ in samples or head size")
+    views = (_heads(q, "q", qs, dtype), _heads(k, "k", ks, dtype), _heads(v, "v", ks, dtype), _heads(o, "o", qs, dtype))
+    stats = _plain(lse, _torch.float32, (qs[0], qs[2], qs[1]), "lse")
+    hd = _heads(do, "do", qs, dtype)
+    at = _device_of(q, k, v, o, lse, do, rule.slopes, rule.documents, rule.q_documents, rule.prefix, *(grads or ()))
+    if grads is None:
+        dq = _torch.empty(qs, dtype=dtype, device=q.device)
+        dk = _torch.empty(ks, dtype=dtype, device=q.device)
+        dv = _torch.empty(ks, dtype=dtype, device=q.device)
+    else:
+        dq, dk, dv = grads
+    lib, need = _lib or load_library(), C.c_size_t()
+    _op_chk(lib, lib.pt_attention_workspace(a, need))
+    ws = _torch.empty((need.value,), dtype=_torch.uint8, device=q.device)
+    _op_chk(lib, _launch(at, lib.pt_attention_bwd, a, *views, stats, hd, _heads(dq, "dq", qs, dtype), _heads(dk, "dk", ks, dtype),
+                         _heads(dv, "dv", ks, dtype), ws.data_ptr(), need.value))
     return dq, dk, dv
-
-
-def _rows(t, name: str):
-    _check(t.dim() == 2 and t.is_contiguous(), f"{name}: [rows, F], contiguous")
 
 
 def gelu8_forward(h):
     """(g, codes, exps): GELU of h [rows, F] and the 8-bit checkpoint of h that gelu8_backward reads."""
-    import torch
-    _rows(h, "h")
+    dtype = _dtype_of(h)
+    if h.dim() != 2 or not h.is_contiguous():
+        _refuse("h: [rows, F], contiguous")
     T, F = h.shape
-    with _On(h) as stream:
-        g = torch.empty_like(h)
-        codes = torch.empty(T, F, dtype=torch.int8, device=h.device)
-        exps = torch.empty(T, (F + 31) // 32, dtype=torch.uint8, device=h.device)
-        lib = load_library()
-        _op_chk(lib, lib.pt_gelu8_fwd(_dtype_of(h), h.data_ptr(), g.data_ptr(), codes.data_ptr(), exps.data_ptr(), T, F, stream))
+    at, dev = _device_of(h), h.device
+    g = _torch.empty((T, F), dtype=h.dtype, device=dev)
+    codes = _torch.empty((T, F), dtype=_torch.int8, device=dev)
+    exps = _torch.empty((T, (F + 31) // 32), dtype=_torch.uint8, device=dev)
+    lib = _lib or load_library()
+    _op_chk(lib, _launch(at, lib.pt_gelu8_fwd, dtype, h.data_ptr(), g.data_ptr(), codes.data_ptr(), exps.data_ptr(), T, F))
     return g, codes, exps
 
 
 def gelu8_backward(codes, exps, dg, want_activation: bool = True, out=None):
     """(dh, g): dg GELU'(x) and GELU(x) (None if not wanted) of the checkpointed x; out: where dh goes (it may be dg itself)."""
-    import torch
-    _rows(dg, "dg")
+    dtype = _dtype_of(dg)
+    if dg.dim() != 2 or not dg.is_contiguous():
+        _refuse("dg: [rows, F], contiguous")
     T, F = dg.shape
-    _check(str(codes.dtype) == "torch.int8" and tuple(codes.shape) == (T, F) and codes.is_contiguous(), f"codes: int8 [{T}, {F}]")
-    _check(str(exps.dtype) == "torch.uint8" and tuple(exps.shape) == (T, (F + 31) // 32) and exps.is_contiguous(),
-           f"exps: uint8 [{T}, {(F + 31) // 32}]")
-    with _On(dg, codes, exps, out) as stream:
-        dh = torch.empty_like(dg) if out is None else out
-        _rows(dh, "out")
-        _check(dh.shape == dg.shape and dh.dtype == dg.dtype, f"out: {dg.dtype} [{T}, {F}]")
-        g = torch.empty_like(dg) if want_activation else None
-        lib = load_library()
-        _op_chk(lib, lib.pt_gelu8_bwd(_dtype_of(dg), codes.data_ptr(), exps.data_ptr(), dg.data_ptr(), dh.data_ptr(),
-                                      g.data_ptr() if want_activation else None, T, F, stream))
+    pc = _plain(codes, _torch.int8, (T, F), "codes")
+    pe = _plain(exps, _torch.uint8, (T, (F + 31) // 32), "exps")
+    at = _device_of(dg, codes, exps, out)
+    dh = _torch.empty((T, F), dtype=dg.dtype, device=dg.device) if out is None else out
+    pd = dh.data_ptr() if out is None else _plain(out, dg.dtype, (T, F), "out")
+    g = _torch.empty((T, F), dtype=dg.dtype, device=dg.device) if want_activation else None
+    lib = _lib or load_library()
+    _op_chk(lib, _launch(at, lib.pt_gelu8_bwd, dtype, pc, pe, dg.data_ptr(), pd, g.data_ptr() if want_activation else None, T, F))
     return dh, g
 
 

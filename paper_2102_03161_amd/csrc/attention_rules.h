@@ -37,131 +37,125 @@ struct RuleRows {
     const int at = g.q0 + i, to = at > prefix - 1 ? at : prefix - 1;
     return to < g.Sk - 1 ? to : g.Sk - 1;
   }
-  __device__ __forceinline__ int qdoc(const AttnRuleArgs& g, int i) const {
-    if (i >= g.Sq) return -2;
-    const int d = q ? q[i] : 0;
-    return d < 0 ? -2 : d;
-  }
-  __device__ __forceinline__ int kdoc(const AttnRuleArgs& g, int j) const {
-    if (j >= g.Sk) return -1;
-    const int d = k ? k[j] : 0;
-    return d < 0 ? -1 : d;
-  }
+  // as they stand in memory (below 0 behind the last row): nothing looks at the value, so that a load for a later tile is not
+  // waited for where it is issued; q_id / k_id turn it into the above
+  __device__ __forceinline__ int q_raw(const AttnRuleArgs& g, int i) const { return i < g.Sq ? (q ? q[i] : 0) : -1; }
+  __device__ __forceinline__ int k_raw(const AttnRuleArgs& g, int j) const { return j < g.Sk ? (k ? k[j] : 0) : -1; }
+  static __device__ __forceinline__ int q_id(int raw) { return raw < 0 ? -2 : raw; }
+  static __device__ __forceinline__ int k_id(int raw) { return raw < 0 ? -1 : raw; }
+  __device__ __forceinline__ int qdoc(const AttnRuleArgs& g, int i) const { return q_id(q_raw(g, i)); }
+  __device__ __forceinline__ int kdoc(const AttnRuleArgs& g, int j) const { return k_id(k_raw(g, j)); }
 };
 
 // Which (sample, head, block of owned rows) a workgroup takes.  Workgroups go to the eight XCDs in turn; the units are dealt so
-// that one XCD gets consecutive ones: the blocks of a head, and the heads that share keys, find them in the same L2.
+// that one XCD gets consecutive ones: the blocks of a head, and the heads that share keys, find them in the same L2.  Blocks with
+// the most to do come first (last_first: the last queries, where the order hides later keys).
 struct RuleUnit {
   int b, h, blk;
-  __device__ __forceinline__ RuleUnit(const AttnRuleArgs& g, int nblk, int heads, int id, int total) {
+  __device__ __forceinline__ RuleUnit(const AttnRuleArgs& g, int nblk, int heads, int id, int total, bool last_first) {
     const int q = total / 8, r = total % 8, x = id % 8;
     const int u = x * q + (x < r ? x : r) + id / 8;
     blk = u % nblk;
+    if (last_first) blk = nblk - 1 - blk;
     h = u / nblk % heads;
     b = u / nblk / heads;
   }
-  __device__ __forceinline__ RuleUnit(const AttnRuleArgs& g, int nblk, int heads) : RuleUnit(g, nblk, heads, blockIdx.x, g.nb * heads * nblk) {}
-  __device__ __forceinline__ RuleUnit(const AttnRuleArgs& g, int nblk, int heads, int id) : RuleUnit(g, nblk, heads, id, g.nb * heads * nblk) {}
 };
 
-// The tiles that a workgroup of four waves visits: entries tile << 8 | full bits << 4 | needed bits.  It lives in LDS behind four
-// waves' ranges and the count.
+// wave-wide minimum of an int, in every lane: DPP row shifts and broadcasts (a chain of LDS permutes takes ten times as long)
+__device__ __forceinline__ int rule_wave_min(int v) {
+#define PT_STEP(ctrl, rows)                                                        \
+  {                                                                               \
+    const int o_ = __builtin_amdgcn_update_dpp(v, v, ctrl, rows, 0xf, false);     \
+    v = o_ < v ? o_ : v;                                                          \
+  }
+  PT_STEP(0x111, 0xf) PT_STEP(0x112, 0xf) PT_STEP(0x114, 0xf) PT_STEP(0x118, 0xf) PT_STEP(0x142, 0xa) PT_STEP(0x143, 0xc)
+#undef PT_STEP
+  return __builtin_amdgcn_readlane(v, 63);
+}
+__device__ __forceinline__ int rule_wave_max(int v) { return ~rule_wave_min(~v); }
+
+// The tiles that a workgroup of four waves visits, each wave owning ROWS rows: entries tile << 8 | whole bits << 4 | needed bits.
+// In LDS: the least and the largest document of each wave's rows and of each tile (the sign of the largest says that padding or
+// several documents are among them), then, in place of the tiles' least, the entries.  A tile is needed by a wave whose range of
+// documents meets its own and whose positions reach it; it is whole if both are one and the same document and all positions of
+// the wave see all of the tile.
+template <int ROWS>
 struct RuleList {
   int* base;
-  __device__ __forceinline__ explicit RuleList(int* p) : base(p) {}
-  static size_t ints(int tiles) { return (size_t)16 + 4 + tiles; }
-  __device__ __forceinline__ int* entries() const { return base + 20; }
-  __device__ __forceinline__ int entry(int it) const { return __builtin_amdgcn_readfirstlane(entries()[it]); }
-  __device__ __forceinline__ int tile(int it) const { return entry(it) >> 8; }
-  __device__ __forceinline__ bool needed(int it, int wave) const { return entry(it) >> wave & 1; }
-  __device__ __forceinline__ bool full(int it, int wave) const { return entry(it) >> (4 + wave) & 1; }
+  int tiles;
+  __device__ __forceinline__ RuleList(int* p, int rows) : base(p), tiles((rows + kRuleTile - 1) / kRuleTile) {}
+  static size_t ints(int tiles) { return (size_t)12 + 2 * tiles + 2; }
+  __device__ __forceinline__ int* lo() const { return base + 12; }              // [tiles + 2]: the loop reads one entry ahead
+  __device__ __forceinline__ int* hi() const { return base + 12 + tiles + 2; }
+  __device__ __forceinline__ int entry(int it) const { return __builtin_amdgcn_readfirstlane(lo()[it]); }
+  static __device__ __forceinline__ bool needed(int e, int wave) { return e >> wave & 1; }
+  static __device__ __forceinline__ bool whole(int e, int wave) { return e >> (4 + wave) & 1; }
 
-  static __device__ __forceinline__ int wave_min(int v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) { const int x = __shfl_xor(v, o, 64); v = x < v ? x : v; }
-    return v;
+  // raw: the lane's document (below 0: padding); in: it is of a row that exists
+  __device__ __forceinline__ void range(int* lo_, int* hi_, int raw, bool in, int lane) const {
+    const bool on = in && raw >= 0;
+    const int least = rule_wave_min(on ? raw : 0x7fffffff), most = rule_wave_max(on ? raw : -1);
+    const bool mixed = least != most || __any(in && !on);
+    if (lane == 0) {
+      *lo_ = least;
+      *hi_ = mixed ? most | (int)0x80000000 : most;
+    }
   }
-  static __device__ __forceinline__ int wave_max(int v) { return ~wave_min(~v); }
-
-  // need / full of one tile for the four waves; d: the lane's row's document (below 0: none), lo / hi: the tile's position bounds
+  // KEYS: tiles of keys for a block of queries, else tiles of queries for a block of keys; own: the lane's row's document.
+  // Returns the number of entries.
   template <bool KEYS>
-  __device__ __forceinline__ int classify(int d, bool in, int lo, int hi) const {
-    int e = 0;
+  __device__ __forceinline__ int build(const AttnRuleArgs& g, const RuleRows& rows, int wave, int lane, int blk, int own, bool own_in) const {
+    const bool docs = rows.q != nullptr;
+    const int n = KEYS ? g.Sk : g.Sq, m = KEYS ? g.Sq : g.Sk;
+    if (docs) {
+      for (int t0 = wave; t0 < tiles; t0 += 32) {       // eight tiles' loads in flight
+        int d[8];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const int dmin = base[4 * w], dmax = base[4 * w + 1], far = base[4 * w + 2], near = base[4 * w + 3];
-      const bool any = __ballot(in && d >= dmin && d <= dmax) != 0;
-      const bool all = __ballot(in ? d != dmin : KEYS) == 0;
-      const bool need = any && (KEYS ? lo <= far : hi >= far);
-      const bool full = need && all && (KEYS ? hi <= near : lo >= near);
-      e |= (need ? 1 : 0) << w | (full ? 1 : 0) << (4 + w);
+        for (int x = 0; x < 8; ++x) {
+          const int r = (t0 + 4 * x) * kRuleTile + lane;
+          d[x] = (KEYS ? rows.k : rows.q)[r < n ? r : n - 1];
+        }
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const int t = t0 + 4 * x;
+          if (t < tiles) range(lo() + t, hi() + t, d[x], t * kRuleTile + lane < n, lane);
+        }
+      }
+      range(base + 2 * wave, base + 2 * wave + 1, own, own_in, lane);
+      __syncthreads();
     }
-    return e;
-  }
-  __device__ __forceinline__ int compact(int nt, int wave, int lane) const {
-    __syncthreads();
     if (wave == 0) {
-      int n = 0;
-      for (int t0 = 0; t0 < nt; t0 += 64) {
-        const int t = t0 + lane;
-        const int e = t < nt ? entries()[t] : 0;
+      int count = 0;
+      for (int t0 = 0; t0 < tiles; t0 += 64) {
+        const int t = t0 + lane, r0 = t * kRuleTile, r1 = r0 + kRuleTile - 1;
+        const int tlo = docs && t < tiles ? lo()[t] : 0, thi_ = docs && t < tiles ? hi()[t] : 0;
+        const int thi = thi_ & 0x7fffffff;
+        const int lim0 = KEYS ? 0 : rows.lim(g, r0), lim1 = KEYS ? 0 : rows.lim(g, r1 < n ? r1 : n - 1);
+        int e = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const int o0 = (blk * 4 + w) * ROWS, o1 = o0 + ROWS - 1 < m ? o0 + ROWS - 1 : m - 1;
+          const int wlo = docs ? base[2 * w] : 0, whi_ = docs ? base[2 * w + 1] : 0, whi = whi_ & 0x7fffffff;
+          bool need = t < tiles && o0 < m && tlo <= whi && wlo <= thi;
+          bool all = thi_ >= 0 && whi_ >= 0 && tlo == wlo;
+          if (KEYS) {
+            need = need && r0 <= rows.lim(g, o1);
+            all = all && r1 <= rows.lim(g, o0);
+          } else {
+            need = need && lim1 >= o0;
+            all = all && lim0 >= o1;
+          }
+          e |= (need ? 1 : 0) << w | (need && all ? 1 : 0) << (4 + w);
+        }
         const uint64_t bits = __ballot(e != 0);
-        if (e) entries()[n + __popcll(bits & ((1ull << lane) - 1))] = t << 8 | e;
-        n += __popcll(bits);
+        if (e) lo()[count + __popcll(bits & ((1ull << lane) - 1))] = t << 8 | e;
+        count += __popcll(bits);
       }
-      if (lane == 0) base[16] = n;
+      if (lane == 0) base[8] = count;
     }
     __syncthreads();
-    return __builtin_amdgcn_readfirstlane(base[16]);
-  }
-  // tiles of keys for the wave's queries (owned by lane; halves hold the same rows).  Ranges: documents of the rows that see
-  // anything, the largest lim (tiles behind it are skipped), and the smallest (tiles in front of it may be whole), the latter -1
-  // where the rows are not all of one document.
-  __device__ __forceinline__ int keys(const AttnRuleArgs& g, const RuleRows& rows, int wave, int lane, bool ok, int lim, int d) const {
-    const bool on = ok && d >= 0;
-    const int dmin = wave_min(on ? d : 0x7fffffff), dmax = wave_max(on ? d : -1);
-    const int far = wave_max(on ? lim : -1);
-    int near = wave_min(on ? lim : 0x7fffffff);
-    if (dmin != dmax || __any(ok && !on)) near = -1;
-    if (lane == 0) { base[4 * wave] = dmin; base[4 * wave + 1] = dmax; base[4 * wave + 2] = far; base[4 * wave + 3] = near; }
-    __syncthreads();
-    const int nt = (g.Sk + kRuleTile - 1) / kRuleTile;
-    for (int t0 = wave * 8; t0 < nt; t0 += 32) {
-      int kd[8];
-#pragma unroll
-      for (int x = 0; x < 8; ++x) kd[x] = rows.kdoc(g, (t0 + x) * kRuleTile + lane);
-#pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        const int j0 = (t0 + x) * kRuleTile;
-        const int e = classify<true>(kd[x], j0 + lane < g.Sk, j0, j0 + kRuleTile - 1);
-        if (lane == 0 && t0 + x < nt) entries()[t0 + x] = e;
-      }
-    }
-    return compact(nt, wave, lane);
-  }
-  // tiles of queries for the wave's keys: documents, the first key's position (a tile whose last query does not reach it is
-  // skipped) and the last one's (a tile whose first query reaches it may be whole)
-  __device__ __forceinline__ int queries(const AttnRuleArgs& g, const RuleRows& rows, int wave, int lane, bool ok, int j, int d) const {
-    const bool on = ok && d >= 0;
-    const int dmin = wave_min(on ? d : 0x7fffffff), dmax = wave_max(on ? d : -1);
-    const int far = wave_min(on ? j : 0x7fffffff);
-    int near = wave_max(on ? j : -1);
-    if (dmin != dmax || __any(ok && !on)) near = 0x7fffffff;
-    if (lane == 0) { base[4 * wave] = dmin; base[4 * wave + 1] = dmax; base[4 * wave + 2] = far; base[4 * wave + 3] = near; }
-    __syncthreads();
-    const int nt = (g.Sq + kRuleTile - 1) / kRuleTile;
-    for (int t0 = wave * 8; t0 < nt; t0 += 32) {
-      int qd[8];
-#pragma unroll
-      for (int x = 0; x < 8; ++x) qd[x] = rows.qdoc(g, (t0 + x) * kRuleTile + lane);
-#pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        const int i0 = (t0 + x) * kRuleTile, i1 = i0 + kRuleTile - 1;
-        const int e = classify<false>(qd[x], i0 + lane < g.Sq, rows.lim(g, i0), rows.lim(g, i1 < g.Sq ? i1 : g.Sq - 1));
-        if (lane == 0 && t0 + x < nt) entries()[t0 + x] = e;
-      }
-    }
-    return compact(nt, wave, lane);
+    return __builtin_amdgcn_readfirstlane(base[8]);
   }
 };
 

@@ -26,10 +26,14 @@ typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 namespace {
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float half_swap(float x) { return __shfl_xor(x, 32, 64); }
+// the value of the lane 32 away
+__device__ __forceinline__ float half_swap(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
 
-// accumulator register v of a 32x32 tile holds tile row 8*(v/4) + 4*half + v%4 (column = lane%32)
-__device__ __forceinline__ int acc_row(int v, int half) { return 8 * (v >> 2) + 4 * half + (v & 3); }
+// accumulator register v of a 32x32 tile holds tile row 8*(v/4) + v%4 + 4*half (column = lane%32)
+constexpr int acc_row(int v) { return 8 * (v >> 2) + (v & 3); }
 __device__ __forceinline__ f32x16 zero16() {
   f32x16 z;
 #pragma unroll
@@ -49,16 +53,9 @@ struct Tile {
   static constexpr int LD = DP + 8;                   // 16-byte row reads without conflicts
   static constexpr int ELEMS = kRuleTile * LD;
   static constexpr int N = kRuleTile * DP / 8 / 256;  // 16-byte pieces per thread
+  static constexpr int RSTEP = 256 / (DP / 8);        // rows between a thread's pieces
   static constexpr int KS = DP / 16;                  // k steps of a product over the head size
   static constexpr int DT = DP / 32;                  // 32-column tiles of the head size
-  static __device__ __forceinline__ int row_of(int tid, int u) { return (tid + 256 * u) / (DP / 8); }
-  static __device__ __forceinline__ int col_of(int tid) { return (tid % (DP / 8)) * 8; }
-  static __device__ __forceinline__ uint4 load(const bf16* p, int64_t ld, int row, int n, int col, int dh) {
-    return row < n && col < dh ? *reinterpret_cast<const uint4*>(p + row * ld + col) : make_uint4(0, 0, 0, 0);
-  }
-  static __device__ __forceinline__ void store(bf16* s, int tid, int u, uint4 x, bool keep) {
-    *reinterpret_cast<uint4*>(s + row_of(tid, u) * LD + col_of(tid)) = keep ? x : make_uint4(0, 0, 0, 0);
-  }
   // the wave's own row as an operand: columns 16 ks + 8 half .. + 7
   static __device__ __forceinline__ void own(const bf16* row, bool ok, int dh, int half, bf16x8 (&f)[KS]) {
 #pragma unroll
@@ -78,6 +75,13 @@ struct Tile {
       acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(p + 16 * ks), f[ks], acc, 0, 0, 0);
     return acc;
   }
+  static __device__ __forceinline__ bf16x8 column(const bf16* q) {
+    typedef __attribute__((address_space(3))) bf16x4 lds4;
+    union { bf16x4 h[2]; bf16x8 v; } t;
+    t.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(q));
+    t.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(q + 8 * LD));
+    return t.v;
+  }
   // acc[dt] (columns 32 dt + .. of the owned rows) += sum over rows r0 .. r0 + 31 of tile row x weight; the transposing LDS read
   // hands a lane four consecutive rows of one column, in the order in which the weights stand in the accumulator
   static __device__ __forceinline__ void add(const bf16* s, int r0, int lane, const f32x16& w, f32x16 (&acc)[DT]) {
@@ -88,14 +92,35 @@ struct Tile {
       const bf16x8 b = pack8(w, 8 * ks2);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        typedef __attribute__((address_space(3))) bf16x4 lds4;
-        const bf16* q = p + 16 * ks2 * LD + 32 * dt;
-        union { bf16x4 h[2]; bf16x8 v; } t;
-        t.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(q));
-        t.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(q + 8 * LD));
-        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.v, b, acc[dt], 0, 0, 0);
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(column(p + 16 * ks2 * LD + 32 * dt), b, acc[dt], 0, 0, 0);
       }
     }
+  }
+  // the same for two weights and two results
+  static __device__ __forceinline__ void add2(const bf16* s, int r0, int lane, const f32x16& w, f32x16 (&acc)[DT], const f32x16& w2, f32x16 (&acc2)[DT]) {
+    const int l16 = lane & 15, grp = lane >> 4;
+    const bf16* p = s + (r0 + 4 * (grp >> 1) + (l16 >> 2)) * LD + 16 * (grp & 1) + 4 * (l16 & 3);
+#pragma unroll
+    for (int ks2 = 0; ks2 < 2; ++ks2) {
+      const bf16x8 b = pack8(w, 8 * ks2), b2 = pack8(w2, 8 * ks2);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const bf16x8 t = column(p + 16 * ks2 * LD + 32 * dt);
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t, b, acc[dt], 0, 0, 0);
+        acc2[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t, b2, acc2[dt], 0, 0, 0);
+      }
+    }
+  }
+  // the wave's own row of another matrix times its operand f, summed over the head size; the same in both halves
+  static __device__ __forceinline__ float own_dot(const bf16* row, bool ok, int dh, int half, const bf16x8 (&f)[KS]) {
+    bf16x8 x[KS];
+    own(row, ok, dh, half, x);
+    float d = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d = fmaf(to_f32(x[ks][e]), to_f32(f[ks][e]), d);
+    return d + half_swap(d);
   }
   static __device__ __forceinline__ void put(bf16* row, int dh, int half, float f, const f32x16 (&acc)[DT]) {
 #pragma unroll
@@ -111,6 +136,71 @@ struct Tile {
   }
 };
 
+// One streamed matrix: this thread's pieces of a tile, loaded while the tile before is multiplied.  Rows behind the last are read
+// as the last one and columns behind the head size as column 0, so that no load hangs on a branch; store() zeroes both, and padding.
+template <int DP>
+struct Stream {
+  typedef Tile<DP> T;
+  const bf16* base;
+  int64_t ld, at;       // at: of the thread's first piece in a whole tile
+  int row, col;
+  bool col_ok;
+  uint4 r[T::N];
+  __device__ __forceinline__ Stream(const HeadView& v, int b, int h, int tid, int dh) {
+    base = static_cast<const bf16*>(v.p) + b * v.b + h * v.h;
+    ld = v.t;
+    row = tid / (DP / 8);
+    col = (tid % (DP / 8)) * 8;
+    col_ok = col < dh;
+    at = row * ld + (col_ok ? col : 0);
+  }
+  __device__ __forceinline__ void load(int r0, int n) {
+    const bf16* p = base + r0 * ld;
+    if (r0 + kRuleTile <= n) {
+#pragma unroll
+      for (int x = 0; x < T::N; ++x) r[x] = *reinterpret_cast<const uint4*>(p + x * T::RSTEP * ld + at);
+    } else {
+#pragma unroll
+      for (int x = 0; x < T::N; ++x) {
+        const int i = row + x * T::RSTEP, last = n - 1 - r0;
+        r[x] = *reinterpret_cast<const uint4*>(p + (i < last ? i : last) * ld + (col_ok ? col : 0));
+      }
+    }
+  }
+  __device__ __forceinline__ void store(bf16* s, const bool (&keep)[T::N]) const {
+#pragma unroll
+    for (int x = 0; x < T::N; ++x)
+      *reinterpret_cast<uint4*>(s + (row + x * T::RSTEP) * T::LD + col) = keep[x] && col_ok ? r[x] : make_uint4(0, 0, 0, 0);
+  }
+};
+// the documents of the same pieces' rows
+template <int DP>
+struct StreamDocs {
+  typedef Tile<DP> T;
+  const int32_t* d;
+  int n, row;
+  int raw[T::N];
+  __device__ __forceinline__ StreamDocs(const int32_t* docs, int n_, int tid) : d(docs), n(n_), row(tid / (DP / 8)) {}
+  __device__ __forceinline__ void load(int r0) {
+    if (d) {
+#pragma unroll
+      for (int x = 0; x < T::N; ++x) {
+        const int i = r0 + row + x * T::RSTEP;
+        raw[x] = d[i < n ? i : n - 1];
+      }
+    }
+  }
+  // keep: the row exists and is no padding; its document (as the owned side compares it) goes to docs unless null
+  __device__ __forceinline__ void finish(int r0, int none, int* docs, bool first, bool (&keep)[T::N]) const {
+#pragma unroll
+    for (int x = 0; x < T::N; ++x) {
+      const int i = row + x * T::RSTEP, v = d ? raw[x] : 0;
+      keep[x] = r0 + i < n && v >= 0;
+      if (first) docs[i] = keep[x] ? v : none;
+    }
+  }
+};
+
 // Scores in the log2 domain.  tanh(x) = 1 - 2 r with r = 1 / (1 + e^2x), which needs no case for large |x|; its derivative
 // 4 r (1 - r) has no cancellation.  The absolute error of 1e-7 cap that this form has near zero is far below a bf16 score's.
 struct Score {
@@ -123,332 +213,367 @@ struct Score {
     sl = g.slopes ? -g.slopes[h] * kLog2e : 0.f;
   }
   __device__ __forceinline__ float bend(float s) const { return __builtin_amdgcn_rcpf(1.f + fast_exp2(s * e1)); }   // r
-  // dist: |position of the query - position of the key|
+  // score + nm; raw: the product, or with a cap bend() of it; dist: position of the query - position of the key, of any sign
   template <int MOD>
-  __device__ __forceinline__ float at(float s, float dist) const {
-    float x = (MOD & 1) ? fmaf(-2.f * a, bend(s), a) : s * c;
-    return (MOD & 2) ? fmaf(sl, dist, x) : x;
+  __device__ __forceinline__ float at(float raw, float dist, float nm) const {
+    const float y = (MOD & 2) ? fmaf(sl, fabsf(dist), nm) : nm;
+    return (MOD & 1) ? fmaf(-2.f * a, raw, y + a) : fmaf(raw, c, y);
   }
 };
+
+// visible pairs of a tile that is not whole, 4 streamed rows at a time
+__device__ __forceinline__ void four(const int* p, int (&x)[4]) {
+  const int4 v = *reinterpret_cast<const int4*>(p);
+  x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+}
 
 // ---------------------------------------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------------------------------------
+// A row's reference m (log2 domain) only has to keep exp2 in range: it is the maximum of the first tile in which the row sees
+// anything, and moves only when a tile's sum passes 2^40.  So a tile whose rows all have one needs no maximum at all.
+constexpr float kGrown = 1099511627776.f;   // 2^40
+
 template <int DP, int MOD>
 __global__ __launch_bounds__(256) void rule_fwd_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   bf16* buf = reinterpret_cast<bf16*>(smem);                                  // [2][K tile, V tile]
   int* kdoc = reinterpret_cast<int*>(buf + 4 * T::ELEMS);                     // [2][64]
-  RuleList list(reinterpret_cast<int*>(kdoc + 2 * kRuleTile));
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  const RuleList<32> list(kdoc + 2 * kRuleTile, g.Sk);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
   const int nqb = (g.Sq + 127) / 128;
-  const RuleUnit u(g, nqb, g.H);
+  const RuleUnit u(g, nqb, g.H, blockIdx.x, gridDim.x, g.order != 0);
   const int b = u.b, h = u.h, hk = h / (g.H / g.Hkv);
   const int i = u.blk * 128 + wave * 32 + (lane & 31);
   const RuleRows rows(g, b);
-  const int lim = rows.lim(g, i), qd = rows.qdoc(g, i);
   const bool ok = i < g.Sq;
-  const int n = list.keys(g, rows, wave, lane, ok, lim, qd);
+  const int lim = rows.lim(g, i), qd = rows.qdoc(g, i);
+  const bool on = ok && qd >= 0;
   bf16x8 qf[T::KS];
-  T::own(static_cast<const bf16*>(g.q.p) + b * g.q.b + (int64_t)i * g.q.t + h * g.q.h, ok && qd >= 0, g.dh, half, qf);
-  const bf16* kp = static_cast<const bf16*>(g.k.p) + b * g.k.b + hk * g.k.h;
-  const bf16* vp = static_cast<const bf16*>(g.v.p) + b * g.v.b + hk * g.v.h;
+  T::own(static_cast<const bf16*>(g.q.p) + b * g.q.b + (int64_t)i * g.q.t + h * g.q.h, on, g.dh, half, qf);
+  const int n = list.build<true>(g, rows, wave, lane, u.blk, qd, ok);
+  Stream<DP> sk(g.k, b, hk, tid, g.dh), sv(g.v, b, hk, tid, g.dh);
+  StreamDocs<DP> sd(rows.k, g.Sk, tid);
   const Score sc(g, h);
   f32x16 o[T::DT];
 #pragma unroll
   for (int dt = 0; dt < T::DT; ++dt) o[dt] = zero16();
-  float m = -1e30f, lsum = 0.f;
-  uint4 rk[T::N], rv[T::N];
-  int rd[T::N];
-  auto load = [&](int it) {
-    const int j0 = list.tile(it) * kRuleTile;
-#pragma unroll
-    for (int x = 0; x < T::N; ++x) {
-      const int j = j0 + T::row_of(tid, x);
-      rk[x] = T::load(kp, g.k.t, j, g.Sk, T::col_of(tid), g.dh);
-      rv[x] = T::load(vp, g.v.t, j, g.Sk, T::col_of(tid), g.dh);
-      rd[x] = rows.kdoc(g, j);
-    }
+  float m = 0.f, lsum = 0.f;
+  auto load = [&](int e) {
+    const int j0 = (e >> 8) * kRuleTile;
+    sd.load(j0);
+    sk.load(j0, g.Sk);
+    sv.load(j0, g.Sk);
   };
-  auto store = [&](int it) {
-    bf16* kb = buf + (it & 1) * 2 * T::ELEMS;
-#pragma unroll
-    for (int x = 0; x < T::N; ++x) {
-      T::store(kb, tid, x, rk[x], rd[x] >= 0);
-      T::store(kb + T::ELEMS, tid, x, rv[x], rd[x] >= 0);
-      if (T::col_of(tid) == 0) kdoc[(it & 1) * kRuleTile + T::row_of(tid, x)] = rd[x];
-    }
+  auto store = [&](int e, int at) {
+    bool keep[T::N];
+    sd.finish((e >> 8) * kRuleTile, -1, kdoc + at * kRuleTile, sk.col == 0, keep);
+    sk.store(buf + at * 2 * T::ELEMS, keep);
+    sv.store(buf + at * 2 * T::ELEMS + T::ELEMS, keep);
   };
-  if (n > 0) { load(0); store(0); }
+  int e = list.entry(0), next = list.entry(1);
+  if (n > 0) { load(e); store(e, 0); }
   for (int it = 0; it < n; ++it) {
     __syncthreads();
-    if (it + 1 < n) load(it + 1);
-    if (list.needed(it, wave)) {
+    if (it + 1 < n) load(next);
+    if (list.needed(e, wave)) {
       const bf16* kb = buf + (it & 1) * 2 * T::ELEMS;
-      const int j0 = list.tile(it) * kRuleTile;
-      const bool full = list.full(it, wave);
+      const int j0 = (e >> 8) * kRuleTile;
+      const float at = (float)(g.q0 + i - j0 - 4 * half);
       f32x16 s[2];
+      // scores less the reference, of the visible pairs; -infinity of the others
+      auto scores = [&]() {
 #pragma unroll
-      for (int st = 0; st < 2; ++st) s[st] = T::dot(kb, 32 * st, lane, qf);
-      const float at = (float)(g.q0 + i - j0);
+        for (int st = 0; st < 2; ++st) {
+          s[st] = T::dot(kb, 32 * st, lane, qf);
 #pragma unroll
-      for (int st = 0; st < 2; ++st)
+          for (int v = 0; v < 16; ++v) s[st][v] = sc.at<MOD>((MOD & 1) ? sc.bend(s[st][v]) : s[st][v], at - (float)(32 * st + acc_row(v)), -m);
+        }
+        if (!list.whole(e, wave)) {
+          const int far = lim - j0 - 4 * half;
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (MOD) s[st][v] = sc.at<MOD>(s[st][v], fabsf(at - (float)(32 * st + acc_row(v, half))));
-      if (!full) {
+          for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4) {
+              int kd[4];
+              four(kdoc + (it & 1) * kRuleTile + 32 * st + 8 * g4 + 4 * half, kd);
+#pragma unroll
+              for (int x = 0; x < 4; ++x) s[st][4 * g4 + x] = kd[x] == qd && 32 * st + 8 * g4 + x <= far ? s[st][4 * g4 + x] : -INFINITY;
+            }
+        }
+      };
+      auto weights = [&](float shift) {
+        float sum = 0.f;
 #pragma unroll
         for (int st = 0; st < 2; ++st)
 #pragma unroll
-          for (int g4 = 0; g4 < 4; ++g4) {
-            const int r0 = 32 * st + 8 * g4 + 4 * half;
-            const int4 kd = *reinterpret_cast<const int4*>(kdoc + (it & 1) * kRuleTile + r0);
-            const int kds[4] = {kd.x, kd.y, kd.z, kd.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[st][4 * g4 + e] = kds[e] == qd && j0 + r0 + e <= lim ? s[st][4 * g4 + e] : -INFINITY;
+          for (int v = 0; v < 16; ++v) {
+            s[st][v] = fast_exp2(s[st][v] - shift);
+            sum += s[st][v];
           }
+        return sum;
+      };
+      bool found = !__any(on && lsum == 0.f);
+      float sum = 0.f;
+      if (found) {
+        scores();
+        sum = weights(0.f);
+        found = !__any(sum > kGrown);
       }
-      float mx = fmaxf(s[0][0], s[1][0]);
+      if (!found) {   // some row has no reference yet, or one that is too low
+        scores();
+        float mx = s[0][0];
 #pragma unroll
-      for (int v = 1; v < 16; ++v) mx = fmaxf(mx, fmaxf(s[0][v], s[1][v]));
-      mx = fmaxf(mx, half_swap(mx));
-      if (!MOD) mx *= sc.c;
-      // the reference maximum only has to keep exp2 in range: it moves when a row's maximum has grown by more than 2^8
-      if (__any(mx > m + 8.f)) {
-        const float mn = mx > m + 8.f ? mx : m;
-        const float alpha = fast_exp2(m - mn);
-        lsum *= alpha;
-        m = mn;
+        for (int v = 1; v < 32; ++v) mx = fmaxf(mx, s[v >> 4][v & 15]);
+        mx = fmaxf(mx, half_swap(mx));
+        const bool move = mx > -INFINITY && (lsum == 0.f || mx > 0.f);
+        const float up = move ? mx : 0.f, alpha = fast_exp2(-up);
+        m += up;
+        lsum *= lsum == 0.f ? 1.f : alpha;
 #pragma unroll
         for (int dt = 0; dt < T::DT; ++dt)
 #pragma unroll
-          for (int v = 0; v < 16; ++v) o[dt][v] *= alpha;
+          for (int v = 0; v < 16; ++v) o[dt][v] *= lsum == 0.f ? 0.f : alpha;
+        sum = weights(up);
       }
+      lsum += sum + half_swap(sum);
 #pragma unroll
-      for (int st = 0; st < 2; ++st) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          s[st][v] = fast_exp2(MOD ? s[st][v] - m : fmaf(s[st][v], sc.c, -m));
-          lsum += s[st][v];
-        }
-        T::add(kb + T::ELEMS, 32 * st, lane, s[st], o);
-      }
+      for (int st = 0; st < 2; ++st) T::add(kb + T::ELEMS, 32 * st, lane, s[st], o);
     }
-    if (it + 1 < n) store(it + 1);
+    if (it + 1 < n) store(next, (it + 1) & 1);
+    e = next;
+    next = list.entry(it + 2 <= list.tiles ? it + 2 : list.tiles);
   }
-  lsum += half_swap(lsum);
   if (!ok) return;
-  T::put(static_cast<bf16*>(const_cast<void*>(g.o.p)) + b * g.o.b + (int64_t)i * g.o.t + h * g.o.h, g.dh, half, lsum > 0.f ? 1.f / lsum : 0.f, o);
-  if (g.lse && half == 0) g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i] = lsum > 0.f ? (m + __log2f(lsum)) * 0.693147180559945f : -INFINITY;
+  T::put(static_cast<bf16*>(const_cast<void*>(g.o.p)) + b * g.o.b + (int64_t)i * g.o.t + h * g.o.h, g.dh, half, lsum == 0.f ? 0.f : 1.f / lsum, o);
+  if (g.lse && half == 0) g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i] = lsum == 0.f ? -INFINITY : (m + __log2f(lsum)) * 0.693147180559945f;
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
-// backward: delta, then one launch whose workgroups take dk / dv of 128 keys (first) or dq of 128 queries
+// backward: dq (128 queries a workgroup), which also leaves each query's delta, then dk and dv (128 keys a workgroup)
 // ---------------------------------------------------------------------------------------------------------------------------
+// delta_i = dO_i . o_i with o rounded to bf16 is off by 2^-9 of |dO||o|, which for a query with few keys, or one that takes most
+// of the weight, is as large as dS itself.  So the pass uses that value d only to centre dP, and takes out what is left of it:
+// with r_i = sum_j p_ij (dP_ij - d_i), the true delta is d_i + r_i, and dq_i = scale (sum_j w_ij (dP_ij - d_i) k_j - r_i sum_j
+// w_ij k_j), w = p (1 - tanh^2): one more product with the keys' fragments that the pass has in registers anyway.
 // p of 1 means a query that sees one key: dS is exactly 0 then, where dP - delta would leave the rounding of two different sums
 constexpr float kOneKey = 1.f - 1.f / 65536.f;
 
 template <int DP, int MOD>
-__device__ __forceinline__ void rule_dq(const AttnRuleArgs& g, int unit, unsigned char* smem) {
+__global__ __launch_bounds__(256) void rule_dq_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   bf16* buf = reinterpret_cast<bf16*>(smem);
   int* kdoc = reinterpret_cast<int*>(buf + 4 * T::ELEMS);
-  RuleList list(reinterpret_cast<int*>(kdoc + 2 * kRuleTile));
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  const RuleList<32> list(kdoc + 2 * kRuleTile, g.Sk);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
   const int nqb = (g.Sq + 127) / 128;
-  const RuleUnit u(g, nqb, g.H, unit);
+  const RuleUnit u(g, nqb, g.H, blockIdx.x, gridDim.x, g.order != 0);
   const int b = u.b, h = u.h, hk = h / (g.H / g.Hkv);
   const int i = u.blk * 128 + wave * 32 + (lane & 31);
   const RuleRows rows(g, b);
   const int lim = rows.lim(g, i), qd = rows.qdoc(g, i);
   const bool ok = i < g.Sq, on = ok && qd >= 0;
-  const int n = list.keys(g, rows, wave, lane, ok, lim, qd);
   bf16x8 qf[T::KS], dof[T::KS];
   T::own(static_cast<const bf16*>(g.q.p) + b * g.q.b + (int64_t)i * g.q.t + h * g.q.h, on, g.dh, half, qf);
   T::own(static_cast<const bf16*>(g.d_o.p) + b * g.d_o.b + (int64_t)i * g.d_o.t + h * g.d_o.h, on, g.dh, half, dof);
-  const bf16* kp = static_cast<const bf16*>(g.k.p) + b * g.k.b + hk * g.k.h;
-  const bf16* vp = static_cast<const bf16*>(g.v.p) + b * g.v.b + hk * g.v.h;
+  const float nlse = on ? -rule_lse2(g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i]) : -INFINITY;
+  const float dl = T::own_dot(static_cast<const bf16*>(g.o.p) + b * g.o.b + (int64_t)i * g.o.t + h * g.o.h, on, g.dh, half, dof);
+  const int n = list.build<true>(g, rows, wave, lane, u.blk, qd, ok);
+  Stream<DP> sk(g.k, b, hk, tid, g.dh), sv(g.v, b, hk, tid, g.dh);
+  StreamDocs<DP> sd(rows.k, g.Sk, tid);
   const Score sc(g, h);
-  const float lse2 = on ? rule_lse2(g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i]) : INFINITY;
-  const float dl = on ? g.delta[((int64_t)b * g.H + h) * g.Sq + i] : 0.f;
-  f32x16 dq[T::DT];
+  f32x16 dq[T::DT], wk[T::DT];
 #pragma unroll
-  for (int dt = 0; dt < T::DT; ++dt) dq[dt] = zero16();
-  uint4 rk[T::N], rv[T::N];
-  int rd[T::N];
-  auto load = [&](int it) {
-    const int j0 = list.tile(it) * kRuleTile;
-#pragma unroll
-    for (int x = 0; x < T::N; ++x) {
-      const int j = j0 + T::row_of(tid, x);
-      rk[x] = T::load(kp, g.k.t, j, g.Sk, T::col_of(tid), g.dh);
-      rv[x] = T::load(vp, g.v.t, j, g.Sk, T::col_of(tid), g.dh);
-      rd[x] = rows.kdoc(g, j);
-    }
+  for (int dt = 0; dt < T::DT; ++dt) { dq[dt] = zero16(); wk[dt] = zero16(); }
+  float rest = 0.f;
+  auto load = [&](int e) {
+    const int j0 = (e >> 8) * kRuleTile;
+    sd.load(j0);
+    sk.load(j0, g.Sk);
+    sv.load(j0, g.Sk);
   };
-  auto store = [&](int it) {
-    bf16* kb = buf + (it & 1) * 2 * T::ELEMS;
-#pragma unroll
-    for (int x = 0; x < T::N; ++x) {
-      T::store(kb, tid, x, rk[x], rd[x] >= 0);
-      T::store(kb + T::ELEMS, tid, x, rv[x], rd[x] >= 0);
-      if (T::col_of(tid) == 0) kdoc[(it & 1) * kRuleTile + T::row_of(tid, x)] = rd[x];
-    }
+  auto store = [&](int e, int at) {
+    bool keep[T::N];
+    sd.finish((e >> 8) * kRuleTile, -1, kdoc + at * kRuleTile, sk.col == 0, keep);
+    sk.store(buf + at * 2 * T::ELEMS, keep);
+    sv.store(buf + at * 2 * T::ELEMS + T::ELEMS, keep);
   };
-  if (n > 0) { load(0); store(0); }
+  int e = list.entry(0), next = list.entry(1);
+  if (n > 0) { load(e); store(e, 0); }
   for (int it = 0; it < n; ++it) {
     __syncthreads();
-    if (it + 1 < n) load(it + 1);
-    if (list.needed(it, wave)) {
+    if (it + 1 < n) load(next);
+    if (list.needed(e, wave)) {
       const bf16* kb = buf + (it & 1) * 2 * T::ELEMS;
-      const int j0 = list.tile(it) * kRuleTile;
-      const bool full = list.full(it, wave);
-      const float at = (float)(g.q0 + i - j0);
+      const int j0 = (e >> 8) * kRuleTile;
+      const bool whole = list.whole(e, wave);
+      const float at = (float)(g.q0 + i - j0 - 4 * half);
+      const int far = lim - j0 - 4 * half;
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
         f32x16 s = T::dot(kb, 32 * st, lane, qf);
-        const f32x16 dp = T::dot(kb + T::ELEMS, 32 * st, lane, dof);
-        float ds[16];
+        f32x16 dp = T::dot(kb + T::ELEMS, 32 * st, lane, dof);
+        f32x16 w;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-          const float x = sc.at<MOD>(s[v], fabsf(at - (float)(32 * st + acc_row(v, half))));
-          const float p = fast_exp2(x - lse2);
-          ds[v] = p * (dp[v] - dl);
-          if (!full) ds[v] = p < kOneKey ? ds[v] : 0.f;
-          if (MOD & 1) { const float r = sc.bend(s[v]); ds[v] *= 4.f * r * (1.f - r); }
+          const float r = (MOD & 1) ? sc.bend(s[v]) : s[v];
+          w[v] = fast_exp2(sc.at<MOD>(r, at - (float)(32 * st + acc_row(v)), nlse));
+          dp[v] -= dl;
+          s[v] = r;
         }
-        if (!full) {
+        if (!whole) {
 #pragma unroll
           for (int g4 = 0; g4 < 4; ++g4) {
-            const int r0 = 32 * st + 8 * g4 + 4 * half;
-            const int4 kd = *reinterpret_cast<const int4*>(kdoc + (it & 1) * kRuleTile + r0);
-            const int kds[4] = {kd.x, kd.y, kd.z, kd.w};
+            int kd[4];
+            four(kdoc + (it & 1) * kRuleTile + 32 * st + 8 * g4 + 4 * half, kd);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) ds[4 * g4 + e] = kds[e] == qd && j0 + r0 + e <= lim ? ds[4 * g4 + e] : 0.f;
+            for (int x = 0; x < 4; ++x) {
+              const int v = 4 * g4 + x;
+              const bool see = kd[x] == qd && 32 * st + 8 * g4 + x <= far;
+              dp[v] = see && !(w[v] >= kOneKey) ? dp[v] : 0.f;
+              w[v] = see ? w[v] : 0.f;
+            }
           }
         }
 #pragma unroll
-        for (int v = 0; v < 16; ++v) s[v] = ds[v];
-        T::add(kb, 32 * st, lane, s, dq);
+        for (int v = 0; v < 16; ++v) {
+          dp[v] *= w[v];
+          rest += dp[v];
+          if (MOD & 1) {
+            const float f = 4.f * s[v] * (1.f - s[v]);
+            dp[v] *= f;
+            w[v] *= f;
+          }
+        }
+        T::add2(kb, 32 * st, lane, dp, dq, w, wk);
       }
     }
-    if (it + 1 < n) store(it + 1);
+    if (it + 1 < n) store(next, (it + 1) & 1);
+    e = next;
+    next = list.entry(it + 2 <= list.tiles ? it + 2 : list.tiles);
   }
-  if (ok) T::put(static_cast<bf16*>(const_cast<void*>(g.dq.p)) + b * g.dq.b + (int64_t)i * g.dq.t + h * g.dq.h, g.dh, half, g.scale, dq);
+  rest += half_swap(rest);
+  if (!ok) return;
+  if (half == 0) g.delta[((int64_t)b * g.H + h) * g.Sq + i] = on ? dl + rest : 0.f;
+#pragma unroll
+  for (int dt = 0; dt < T::DT; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) dq[dt][v] = fmaf(-rest, wk[dt][v], dq[dt][v]);
+  T::put(static_cast<bf16*>(const_cast<void*>(g.dq.p)) + b * g.dq.b + (int64_t)i * g.dq.t + h * g.dq.h, g.dh, half, g.scale, dq);
 }
 
 template <int DP, int MOD>
-__device__ __forceinline__ void rule_dkv(const AttnRuleArgs& g, int unit, unsigned char* smem) {
+__global__ __launch_bounds__(256) void rule_dkv_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   bf16* buf = reinterpret_cast<bf16*>(smem);                                  // [2][Q tile, dO tile]
-  float* stat = reinterpret_cast<float*>(buf + 4 * T::ELEMS);                 // [2][lse, delta][64]
+  float* stat = reinterpret_cast<float*>(buf + 4 * T::ELEMS);                 // [2][-lse, delta][64]
   int* info = reinterpret_cast<int*>(stat + 4 * kRuleTile);                   // [2][document, lim][64]
-  RuleList list(info + 4 * kRuleTile);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  const RuleList<32> list(info + 4 * kRuleTile, g.Sq);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
   const int nkb = (g.Sk + 127) / 128, G = g.H / g.Hkv;
-  const RuleUnit u(g, nkb, g.Hkv, unit);
+  const RuleUnit u(g, nkb, g.Hkv, blockIdx.x, gridDim.x, false);
   const int b = u.b, hk = u.h;
   const int j = u.blk * 128 + wave * 32 + (lane & 31);
   const RuleRows rows(g, b);
   const int kd = rows.kdoc(g, j);
   const bool ok = j < g.Sk, on = ok && kd >= 0;
-  const int n = list.queries(g, rows, wave, lane, ok, j, kd);
   bf16x8 kf[T::KS], vf[T::KS];
   T::own(static_cast<const bf16*>(g.k.p) + b * g.k.b + (int64_t)j * g.k.t + hk * g.k.h, on, g.dh, half, kf);
   T::own(static_cast<const bf16*>(g.v.p) + b * g.v.b + (int64_t)j * g.v.t + hk * g.v.h, on, g.dh, half, vf);
+  const int n = list.build<false>(g, rows, wave, lane, u.blk, kd, ok);
   f32x16 dk[T::DT], dv[T::DT];
 #pragma unroll
   for (int dt = 0; dt < T::DT; ++dt) { dk[dt] = zero16(); dv[dt] = zero16(); }
-  uint4 rq[T::N], ro[T::N];
-  int rd[T::N];
-  float rl = 0.f, rdl = 0.f;
-  int rid = 0, rlim = 0;
-  auto load = [&](int it) {
-    const int h = hk * G + it / n, i0 = list.tile(it % n) * kRuleTile;
-    const bf16* qp = static_cast<const bf16*>(g.q.p) + b * g.q.b + h * g.q.h;
-    const bf16* op = static_cast<const bf16*>(g.d_o.p) + b * g.d_o.b + h * g.d_o.h;
-#pragma unroll
-    for (int x = 0; x < T::N; ++x) {
-      const int i = i0 + T::row_of(tid, x);
-      rq[x] = T::load(qp, g.q.t, i, g.Sq, T::col_of(tid), g.dh);
-      ro[x] = T::load(op, g.d_o.t, i, g.Sq, T::col_of(tid), g.dh);
-      rd[x] = rows.qdoc(g, i);
+  const int first = list.entry(0);
+  // the heads that share these keys, one after the other
+  for (int h = hk * G; h < hk * G + G; ++h) {
+    Stream<DP> sq(g.q, b, h, tid, g.dh), so(g.d_o, b, h, tid, g.dh);
+    StreamDocs<DP> sd(rows.q, g.Sq, tid);
+    const Score sc(g, h);
+    const float* lse = g.lse + (int64_t)b * g.lse_b + (int64_t)h * g.lse_h;
+    const float* delta = g.delta + ((int64_t)b * g.H + h) * g.Sq;
+    float rl = 0.f, rdl = 0.f;
+    auto load = [&](int e) {
+      const int i0 = (e >> 8) * kRuleTile;
+      sd.load(i0);
+      if (tid < kRuleTile) {
+        const int r = i0 + tid < g.Sq ? i0 + tid : g.Sq - 1;
+        rl = lse[r];
+        rdl = delta[r];
+      }
+      sq.load(i0, g.Sq);
+      so.load(i0, g.Sq);
+    };
+    auto store = [&](int e, int at) {
+      const int i0 = (e >> 8) * kRuleTile;
+      bool keep[T::N];
+      sd.finish(i0, -2, info + at * 2 * kRuleTile, sq.col == 0, keep);
+      if (tid < kRuleTile) {
+        // a row behind the last has probability 0; so has one that sees nothing (padding among them)
+        stat[at * 2 * kRuleTile + tid] = i0 + tid < g.Sq ? -rule_lse2(rl) : -INFINITY;
+        stat[at * 2 * kRuleTile + kRuleTile + tid] = rdl;
+        info[at * 2 * kRuleTile + kRuleTile + tid] = rows.lim(g, i0 + tid);
+      }
+      sq.store(buf + at * 2 * T::ELEMS, keep);
+      so.store(buf + at * 2 * T::ELEMS + T::ELEMS, keep);
+    };
+    int e = first, next = list.entry(1);
+    if (n > 0) {
+      if (h > hk * G) __syncthreads();   // the last tile of the head before may still be read
+      load(e);
+      store(e, 0);
     }
-    if (tid < kRuleTile) {
-      const int i = i0 + tid;
-      const bool in = i < g.Sq;
-      rid = rows.qdoc(g, i);
-      rlim = rows.lim(g, i);
-      rl = in ? rule_lse2(g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i]) : INFINITY;
-      rdl = in ? g.delta[((int64_t)b * g.H + h) * g.Sq + i] : 0.f;
-    }
-  };
-  auto store = [&](int it) {
-    bf16* qb = buf + (it & 1) * 2 * T::ELEMS;
+    for (int it = 0; it < n; ++it) {
+      __syncthreads();
+      if (it + 1 < n) load(next);
+      if (list.needed(e, wave)) {
+        const bf16* qb = buf + (it & 1) * 2 * T::ELEMS;
+        const float* st2 = stat + (it & 1) * 2 * kRuleTile;
+        const int* inf = info + (it & 1) * 2 * kRuleTile;
+        const bool whole = list.whole(e, wave);
+        const float at = (float)(g.q0 + (e >> 8) * kRuleTile - j + 4 * half);
 #pragma unroll
-    for (int x = 0; x < T::N; ++x) {
-      T::store(qb, tid, x, rq[x], rd[x] >= 0);
-      T::store(qb + T::ELEMS, tid, x, ro[x], rd[x] >= 0);
-    }
-    if (tid < kRuleTile) {
-      const int at = (it & 1) * 2 * kRuleTile + tid;
-      stat[at] = rid >= 0 ? rl : INFINITY;
-      stat[at + kRuleTile] = rdl;
-      info[at] = rid;
-      info[at + kRuleTile] = rlim;
-    }
-  };
-  const int total = n * G;
-  if (total > 0) { load(0); store(0); }
-  for (int it = 0; it < total; ++it) {
-    __syncthreads();
-    if (it + 1 < total) load(it + 1);
-    const int item = it % n;
-    if (list.needed(item, wave)) {
-      const bf16* qb = buf + (it & 1) * 2 * T::ELEMS;
-      const float* st2 = stat + (it & 1) * 2 * kRuleTile;
-      const int* inf = info + (it & 1) * 2 * kRuleTile;
-      const Score sc(g, hk * G + it / n);
-      const bool full = list.full(item, wave);
-      const float at = (float)(g.q0 + list.tile(item) * kRuleTile - j);
+        for (int st = 0; st < 2; ++st) {
+          f32x16 s = T::dot(qb, 32 * st, lane, kf);
+          f32x16 ds = T::dot(qb + T::ELEMS, 32 * st, lane, vf);
 #pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        f32x16 s = T::dot(qb, 32 * st, lane, kf);
-        f32x16 ds = T::dot(qb + T::ELEMS, 32 * st, lane, vf);
+          for (int g4 = 0; g4 < 4; ++g4) {
+            const int r0 = 32 * st + 8 * g4 + 4 * half;
+            const float4 l4 = *reinterpret_cast<const float4*>(st2 + r0);
+            const float4 d4 = *reinterpret_cast<const float4*>(st2 + kRuleTile + r0);
+            const float nl[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
-        for (int g4 = 0; g4 < 4; ++g4) {
-          const int r0 = 32 * st + 8 * g4 + 4 * half;
-          const float4 l4 = *reinterpret_cast<const float4*>(st2 + r0);
-          const float4 d4 = *reinterpret_cast<const float4*>(st2 + kRuleTile + r0);
-          const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
-          float p[4], d[4];
+            for (int x = 0; x < 4; ++x) {
+              const int v = 4 * g4 + x;
+              const float r = (MOD & 1) ? sc.bend(s[v]) : s[v];
+              s[v] = fast_exp2(sc.at<MOD>(r, at + (float)(32 * st + acc_row(v)), nl[x]));
+              ds[v] = s[v] * (ds[v] - dl[x]);
+              if (MOD & 1) ds[v] *= 4.f * r * (1.f - r);
+            }
+            if (!whole) {
+              int qd[4], lm[4];
+              four(inf + r0, qd);
+              four(inf + kRuleTile + r0, lm);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int v = 4 * g4 + e;
-            p[e] = fast_exp2(sc.at<MOD>(s[v], fabsf(at + (float)(r0 + e))) - ls[e]);
-            d[e] = p[e] * (ds[v] - dl[e]);
-            if (MOD & 1) { const float r = sc.bend(s[v]); d[e] *= 4.f * r * (1.f - r); }
-          }
-          if (!full) {
-            const int4 qd4 = *reinterpret_cast<const int4*>(inf + r0);
-            const int4 lm4 = *reinterpret_cast<const int4*>(inf + kRuleTile + r0);
-            const int qds[4] = {qd4.x, qd4.y, qd4.z, qd4.w}, lms[4] = {lm4.x, lm4.y, lm4.z, lm4.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const bool see = qds[e] == kd && j <= lms[e];
-              d[e] = see && p[e] < kOneKey ? d[e] : 0.f;
-              p[e] = see ? p[e] : 0.f;
+              for (int x = 0; x < 4; ++x) {
+                const int v = 4 * g4 + x;
+                const bool see = qd[x] == kd && j <= lm[x];
+                ds[v] = see && !(s[v] >= kOneKey) ? ds[v] : 0.f;
+                s[v] = see ? s[v] : 0.f;
+              }
             }
           }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) { s[4 * g4 + e] = p[e]; ds[4 * g4 + e] = d[e]; }
+          T::add(qb + T::ELEMS, 32 * st, lane, s, dv);
+          T::add(qb, 32 * st, lane, ds, dk);
         }
-        T::add(qb + T::ELEMS, 32 * st, lane, s, dv);
-        T::add(qb, 32 * st, lane, ds, dk);
       }
+      if (it + 1 < n) store(next, (it + 1) & 1);
+      e = next;
+      next = list.entry(it + 2 <= list.tiles ? it + 2 : list.tiles);
     }
-    if (it + 1 < total) store(it + 1);
   }
   if (ok) {
     T::put(static_cast<bf16*>(const_cast<void*>(g.dk.p)) + b * g.dk.b + (int64_t)j * g.dk.t + hk * g.dk.h, g.dh, half, g.scale, dk);
@@ -456,35 +581,25 @@ __device__ __forceinline__ void rule_dkv(const AttnRuleArgs& g, int unit, unsign
   }
 }
 
-template <int DP, int MOD>
-__global__ __launch_bounds__(256) void rule_bwd_kernel(AttnRuleArgs g, int ndkv) {
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  if ((int)blockIdx.x < ndkv) rule_dkv<DP, MOD>(g, blockIdx.x, smem);
-  else rule_dq<DP, MOD>(g, blockIdx.x - ndkv, smem);
-}
-
 template <int DP>
-size_t lds_bytes(int Sq, int Sk, bool bwd) {
-  const int nt = (std::max(bwd ? Sq : 0, Sk) + kRuleTile - 1) / kRuleTile;
-  return (size_t)4 * Tile<DP>::ELEMS * 2 + (bwd ? 8 : 2) * kRuleTile * 4 + RuleList::ints(nt) * 4;
+size_t lds_bytes(int streamed, bool dkv) {
+  return (size_t)4 * Tile<DP>::ELEMS * 2 + (dkv ? 8 : 2) * kRuleTile * 4 + RuleList<32>::ints((streamed + kRuleTile - 1) / kRuleTile) * 4;
 }
-
+template <typename K>
+hipError_t launch(K kernel, int blocks, size_t lds, const AttnRuleArgs& g, hipStream_t st) {
+  if (blocks == 0) return hipSuccess;
+  PT_RULE_LDS(kernel, lds);
+  hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), lds, st, g);
+  return hipGetLastError();
+}
 template <int DP, int MOD>
 hipError_t launch_fwd(const AttnRuleArgs& g, hipStream_t st) {
-  const size_t lds = lds_bytes<DP>(g.Sq, g.Sk, false);
-  const int blocks = g.nb * g.H * ((g.Sq + 127) / 128);
-  PT_RULE_LDS((rule_fwd_kernel<DP, MOD>), lds);
-  hipLaunchKernelGGL((rule_fwd_kernel<DP, MOD>), dim3(blocks), dim3(256), lds, st, g);
-  return hipGetLastError();
+  return launch(rule_fwd_kernel<DP, MOD>, g.nb * g.H * ((g.Sq + 127) / 128), lds_bytes<DP>(g.Sk, false), g, st);
 }
 template <int DP, int MOD>
 hipError_t launch_bwd(const AttnRuleArgs& g, hipStream_t st) {
-  const size_t lds = lds_bytes<DP>(g.Sq, g.Sk, true);
-  const int ndkv = g.nb * g.Hkv * ((g.Sk + 127) / 128), ndq = g.nb * g.H * ((g.Sq + 127) / 128);
-  if (ndkv + ndq == 0) return hipSuccess;
-  PT_RULE_LDS((rule_bwd_kernel<DP, MOD>), lds);
-  hipLaunchKernelGGL((rule_bwd_kernel<DP, MOD>), dim3(ndkv + ndq), dim3(256), lds, st, g, ndkv);
-  return hipGetLastError();
+  const hipError_t e = launch(rule_dq_kernel<DP, MOD>, g.nb * g.H * ((g.Sq + 127) / 128), lds_bytes<DP>(g.Sk, false), g, st);
+  return e != hipSuccess ? e : launch(rule_dkv_kernel<DP, MOD>, g.nb * g.Hkv * ((g.Sk + 127) / 128), lds_bytes<DP>(g.Sq, true), g, st);
 }
 template <int DP>
 hipError_t by_mod(const AttnRuleArgs& g, bool bwd, hipStream_t st) {
@@ -502,10 +617,6 @@ hipError_t attention_rule_fwd(int dt, const AttnRuleArgs& g, hipStream_t st) {
   return dt ? attention_rule_bf16(g, false, st) : attention_rule_f32(g, false, st);
 }
 hipError_t attention_rule_bwd(int dt, const AttnRuleArgs& g, hipStream_t st) {
-  if (g.Sq > 0) {   // (without queries the launch below writes zeros)
-    const hipError_t e = attention_rule_delta(dt, g, st);
-    if (e != hipSuccess) return e;
-  }
   return dt ? attention_rule_bf16(g, true, st) : attention_rule_f32(g, true, st);
 }
 

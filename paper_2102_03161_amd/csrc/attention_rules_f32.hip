@@ -1,5 +1,5 @@
 // Attention under a rule in fp32 on the fp32 matrix instructions (the formulas, the masks and the list of tiles are those of
-// attention_rules.hip; the tiles and fragments those of attention_f32_tile.h), and delta_i = dO_i . o_i for both types.
+// attention_rules.hip; the tiles and fragments those of attention_f32_tile.h).
 //
 // A wave owns 16 rows, a workgroup 64; the other side streams through LDS in tiles of 64 rows.  Bound by the fp32 matrix rate.
 #include "attention_rules.h"
@@ -46,15 +46,15 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_fwd_f32_kernel(Attn
   float* xs = reinterpret_cast<float*>(smem);
   float* ys = xs + A::FLOATS;
   int* kdoc = reinterpret_cast<int*>(ys + A::FLOATS);
-  RuleList list(kdoc + kRuleTile);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, gr = lane >> 4, l = lane & 15;
-  const RuleUnit u(g, (g.Sq + 63) / 64, g.H);
+  const RuleList<16> list(kdoc + kRuleTile, g.Sk);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), gr = lane >> 4, l = lane & 15;
+  const RuleUnit u(g, (g.Sq + 63) / 64, g.H, blockIdx.x, gridDim.x, g.order != 0);
   const int b = u.b, h = u.h, hk = h / (g.H / g.Hkv);
   const int i = u.blk * 64 + wave * 16 + l;
   const RuleRows rows(g, b);
   const int lim = rows.lim(g, i), qd = rows.qdoc(g, i);
   const bool ok = i < g.Sq, on = ok && qd >= 0;
-  const int n = list.keys(g, rows, wave, lane, ok, lim, qd);
+  const int n = list.build<true>(g, rows, wave, lane, u.blk, qd, ok);
   const float* kp = static_cast<const float*>(g.k.p) + b * g.k.b + hk * g.k.h;
   const float* vp = static_cast<const float*>(g.v.p) + b * g.v.b + hk * g.v.h;
   const ScoreF sc(g, h);
@@ -65,22 +65,22 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_fwd_f32_kernel(Attn
   float m = -1e30f, sum = 0.f;
   int rd = 0;
   auto load = [&](int it) {
-    const int j0 = list.tile(it) * kRuleTile;
+    const int j0 = (list.entry(it) >> 8) * kRuleTile;
     A::load(kp, g.k.t, j0, g.Sk, g.dh, tid, rk);
     A::load(vp, g.v.t, j0, g.Sk, g.dh, tid, rv);
-    if (tid < kRuleTile) rd = rows.kdoc(g, j0 + tid);
+    if (tid < kRuleTile) rd = rows.k_raw(g, j0 + tid);
   };
   if (n > 0) load(0);
   for (int it = 0; it < n; ++it) {
     __syncthreads();
-    if (tid < kRuleTile) kdoc[tid] = rd;
+    if (tid < kRuleTile) kdoc[tid] = RuleRows::k_id(rd);
     __syncthreads();
     rule_store<A>(xs, tid, rk, kdoc);
     rule_store<A>(ys, tid, rv, kdoc);
     __syncthreads();
     if (it + 1 < n) load(it + 1);
-    if (!list.needed(it, wave)) continue;
-    const int j0 = list.tile(it) * kRuleTile;
+    if (!list.needed(list.entry(it), wave)) continue;
+    const int j0 = (list.entry(it) >> 8) * kRuleTile;
     const float at = (float)(g.q0 + i - j0);
     f32x4 s[4];
     float mx = m;
@@ -131,19 +131,19 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
   float* ys = xs + A::FLOATS;
   float* ls = ys + A::FLOATS;                            // [lse][delta]
   int* docs = reinterpret_cast<int*>(ls + 2 * kRuleTile);   // [document][lim]
-  RuleList list(docs + 2 * kRuleTile);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, gr = lane >> 4, l = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), gr = lane >> 4, l = lane & 15;
   f32x4 rx[A::N4], ry[A::N4], a0[A::NF], a1[A::NF], ax[A::NF];
 #pragma unroll
   for (int x = 0; x < A::NF; ++x) ax[x] = f32x4{0.f, 0.f, 0.f, 0.f};
   if ((int)blockIdx.x >= ndkv) {   // dq of 64 queries
-    const RuleUnit u(g, (g.Sq + 63) / 64, g.H, blockIdx.x - ndkv);
+    const RuleList<16> list(docs + 2 * kRuleTile, g.Sk);
+    const RuleUnit u(g, (g.Sq + 63) / 64, g.H, blockIdx.x - ndkv, gridDim.x - ndkv, g.order != 0);
     const int b = u.b, h = u.h, hk = h / (g.H / g.Hkv);
     const int i = u.blk * 64 + wave * 16 + l;
     const RuleRows rows(g, b);
     const int lim = rows.lim(g, i), qd = rows.qdoc(g, i);
     const bool ok = i < g.Sq, on = ok && qd >= 0;
-    const int n = list.keys(g, rows, wave, lane, ok, lim, qd);
+    const int n = list.build<true>(g, rows, wave, lane, u.blk, qd, ok);
     A::own(static_cast<const float*>(g.q.p) + b * g.q.b + h * g.q.h, g.q.t, on ? i : g.Sq, g.Sq, g.dh, gr, 1.f, a0);
     A::own(static_cast<const float*>(g.d_o.p) + b * g.d_o.b + h * g.d_o.h, g.d_o.t, on ? i : g.Sq, g.Sq, g.dh, gr, 1.f, a1);
     const float* kp = static_cast<const float*>(g.k.p) + b * g.k.b + hk * g.k.h;
@@ -153,22 +153,22 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
     const float dl = on ? g.delta[((int64_t)b * g.H + h) * g.Sq + i] : 0.f;
     int rd = 0;
     auto load = [&](int it) {
-      const int j0 = list.tile(it) * kRuleTile;
+      const int j0 = (list.entry(it) >> 8) * kRuleTile;
       A::load(kp, g.k.t, j0, g.Sk, g.dh, tid, rx);
       A::load(vp, g.v.t, j0, g.Sk, g.dh, tid, ry);
-      if (tid < kRuleTile) rd = rows.kdoc(g, j0 + tid);
+      if (tid < kRuleTile) rd = rows.k_raw(g, j0 + tid);
     };
     if (n > 0) load(0);
     for (int it = 0; it < n; ++it) {
       __syncthreads();
-      if (tid < kRuleTile) docs[tid] = rd;
+      if (tid < kRuleTile) docs[tid] = RuleRows::k_id(rd);
       __syncthreads();
       rule_store<A>(xs, tid, rx, docs);
       rule_store<A>(ys, tid, ry, docs);
       __syncthreads();
       if (it + 1 < n) load(it + 1);
-      if (!list.needed(it, wave)) continue;
-      const int j0 = list.tile(it) * kRuleTile;
+      if (!list.needed(list.entry(it), wave)) continue;
+      const int j0 = (list.entry(it) >> 8) * kRuleTile;
       const float at = (float)(g.q0 + i - j0);
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
           const int r = 16 * x + 4 * gr + v;
           float bent;
           const float p = __builtin_amdgcn_exp2f(sc.at(s[v], fabsf(at - (float)r), &bent) - lw);
-          const bool see = docs[r] == qd && j0 + r <= lim && p < kOneKeyF;
+          const bool see = docs[r] == qd && j0 + r <= lim && !(p >= kOneKeyF);
           s[v] = see ? p * (dp[v] - dl) * (1.f - bent * bent) : 0.f;
         }
         A::add(xs, 16 * x, l, gr, s, ax);
@@ -190,13 +190,14 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
   }
   // dk and dv of 64 keys
   const int G = g.H / g.Hkv;
-  const RuleUnit u(g, (g.Sk + 63) / 64, g.Hkv, blockIdx.x);
+  const RuleList<16> list(docs + 2 * kRuleTile, g.Sq);
+  const RuleUnit u(g, (g.Sk + 63) / 64, g.Hkv, blockIdx.x, ndkv, false);
   const int b = u.b, hk = u.h;
   const int j = u.blk * 64 + wave * 16 + l;
   const RuleRows rows(g, b);
   const int kd = rows.kdoc(g, j);
   const bool ok = j < g.Sk, on = ok && kd >= 0;
-  const int n = list.queries(g, rows, wave, lane, ok, j, kd);
+  const int n = list.build<false>(g, rows, wave, lane, u.blk, kd, ok);
   A::own(static_cast<const float*>(g.k.p) + b * g.k.b + hk * g.k.h, g.k.t, on ? j : g.Sk, g.Sk, g.dh, gr, 1.f, a0);
   A::own(static_cast<const float*>(g.v.p) + b * g.v.b + hk * g.v.h, g.v.t, on ? j : g.Sk, g.Sk, g.dh, gr, 1.f, a1);
   f32x4 ay[A::NF];
@@ -205,14 +206,14 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
   int rd = 0, rlim = 0;
   float rl = 0.f, rdl = 0.f;
   auto load = [&](int it) {
-    const int h = hk * G + it / n, i0 = list.tile(it % n) * kRuleTile;
+    const int h = hk * G + it / n, i0 = (list.entry(it % n) >> 8) * kRuleTile;
     A::load(static_cast<const float*>(g.q.p) + b * g.q.b + h * g.q.h, g.q.t, i0, g.Sq, g.dh, tid, rx);
     A::load(static_cast<const float*>(g.d_o.p) + b * g.d_o.b + h * g.d_o.h, g.d_o.t, i0, g.Sq, g.dh, tid, ry);
     if (tid < kRuleTile) {
       const int i = i0 + tid;
-      rd = rows.qdoc(g, i);
+      rd = rows.q_raw(g, i);
       rlim = rows.lim(g, i);
-      rl = i < g.Sq && rd >= 0 ? rule_lse2(g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i]) : INFINITY;
+      rl = i < g.Sq ? g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i] : -INFINITY;
       rdl = i < g.Sq ? g.delta[((int64_t)b * g.H + h) * g.Sq + i] : 0.f;
     }
   };
@@ -220,16 +221,16 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
   if (total > 0) load(0);
   for (int it = 0; it < total; ++it) {
     __syncthreads();
-    if (tid < kRuleTile) { docs[tid] = rd; docs[kRuleTile + tid] = rlim; ls[tid] = rl; ls[kRuleTile + tid] = rdl; }
+    if (tid < kRuleTile) { docs[tid] = RuleRows::q_id(rd); docs[kRuleTile + tid] = rlim; ls[tid] = rd >= 0 ? rule_lse2(rl) : INFINITY; ls[kRuleTile + tid] = rdl; }
     __syncthreads();
     rule_store<A>(xs, tid, rx, docs);
     rule_store<A>(ys, tid, ry, docs);
     __syncthreads();
     if (it + 1 < total) load(it + 1);
     const int item = it % n;
-    if (!list.needed(item, wave)) continue;
+    if (!list.needed(list.entry(item), wave)) continue;
     const ScoreF sc(g, hk * G + it / n);
-    const float at = (float)(g.q0 + list.tile(item) * kRuleTile - j);
+    const float at = (float)(g.q0 + (list.entry(item) >> 8) * kRuleTile - j);
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       f32x4 p = A::dot(xs, 16 * x, l, gr, a0);
@@ -241,7 +242,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
         const float e = __builtin_amdgcn_exp2f(sc.at(p[v], fabsf(at + (float)r), &bent) - ls[r]);
         const bool see = docs[r] == kd && j <= docs[kRuleTile + r];
         p[v] = see ? e : 0.f;
-        ds[v] = see && e < kOneKeyF ? e * (ds[v] - ls[kRuleTile + r]) * (1.f - bent * bent) : 0.f;
+        ds[v] = see && !(e >= kOneKeyF) ? e * (ds[v] - ls[kRuleTile + r]) * (1.f - bent * bent) : 0.f;
       }
       A::add(ys, 16 * x, l, gr, p, ay);
       A::add(xs, 16 * x, l, gr, ds, ax);
@@ -255,7 +256,6 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
 
 // delta[b, h, i] = dO . o of one query and head, 0 for padding (whose rows may hold anything).  16 lanes a row; rows are taken
 // with the heads next to each other, as a packed layout has them.
-template <typename T>
 __global__ __launch_bounds__(256) void rule_delta_kernel(AttnRuleArgs g) {
   const int64_t r = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), total = (int64_t)g.nb * g.Sq * g.H;
   if (r >= total) return;
@@ -263,8 +263,8 @@ __global__ __launch_bounds__(256) void rule_delta_kernel(AttnRuleArgs g) {
   const int64_t t = r / g.H;
   const int i = (int)(t % g.Sq), b = (int)(t / g.Sq);
   const RuleRows rows(g, b);
-  const T* o = static_cast<const T*>(g.o.p) + b * g.o.b + (int64_t)i * g.o.t + h * g.o.h;
-  const T* d = static_cast<const T*>(g.d_o.p) + b * g.d_o.b + (int64_t)i * g.d_o.t + h * g.d_o.h;
+  const float* o = static_cast<const float*>(g.o.p) + b * g.o.b + (int64_t)i * g.o.t + h * g.o.h;
+  const float* d = static_cast<const float*>(g.d_o.p) + b * g.d_o.b + (int64_t)i * g.d_o.t + h * g.d_o.h;
   float s = 0.f;
   for (int c = 4 * l; c < g.dh; c += 64) {
     const f32x4 a = load4(o + c), e = load4(d + c);
@@ -279,7 +279,7 @@ __global__ __launch_bounds__(256) void rule_delta_kernel(AttnRuleArgs g) {
 template <int DP>
 hipError_t launch_f32(const AttnRuleArgs& g, bool bwd, hipStream_t st) {
   const int nt = ((bwd && g.Sq > g.Sk ? g.Sq : g.Sk) + kRuleTile - 1) / kRuleTile;
-  const size_t lds = (size_t)2 * AttnTile<float, DP>::FLOATS * 4 + (bwd ? 4 : 1) * kRuleTile * 4 + RuleList::ints(nt) * 4;
+  const size_t lds = (size_t)2 * AttnTile<float, DP>::FLOATS * 4 + (bwd ? 4 : 1) * kRuleTile * 4 + RuleList<16>::ints(nt) * 4;
   const int nq = g.nb * g.H * ((g.Sq + 63) / 64), nk = g.nb * g.Hkv * ((g.Sk + 63) / 64);
   if ((bwd ? nk + nq : nq) == 0) return hipSuccess;
   if (bwd) PT_RULE_LDS(rule_bwd_f32_kernel<DP>, lds);
@@ -292,17 +292,15 @@ hipError_t launch_f32(const AttnRuleArgs& g, bool bwd, hipStream_t st) {
 }  // namespace
 
 hipError_t attention_rule_f32(const AttnRuleArgs& g, bool bwd, hipStream_t st) {
+  if (bwd && g.Sq > 0 && g.nb > 0) {   // (without queries the launch below writes zeros)
+    hipLaunchKernelGGL(rule_delta_kernel, dim3((unsigned)(((int64_t)g.nb * g.Sq * g.H + 15) / 16)), dim3(256), 0, st, g);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   if (g.dh <= 16) return launch_f32<16>(g, bwd, st);
   if (g.dh <= 32) return launch_f32<32>(g, bwd, st);
   if (g.dh <= 64) return launch_f32<64>(g, bwd, st);
   return launch_f32<128>(g, bwd, st);
-}
-
-hipError_t attention_rule_delta(int dt, const AttnRuleArgs& g, hipStream_t st) {
-  const int blocks = (int)(((int64_t)g.nb * g.Sq * g.H + 15) / 16);
-  if (dt) hipLaunchKernelGGL(rule_delta_kernel<bf16>, dim3(blocks), dim3(256), 0, st, g);
-  else hipLaunchKernelGGL(rule_delta_kernel<float>, dim3(blocks), dim3(256), 0, st, g);
-  return hipGetLastError();
 }
 
 }  // namespace pt

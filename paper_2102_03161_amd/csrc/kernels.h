@@ -80,7 +80,6 @@ hipError_t attention_rule_fwd(int dt, const AttnRuleArgs& g, hipStream_t st);
 hipError_t attention_rule_bwd(int dt, const AttnRuleArgs& g, hipStream_t st);
 hipError_t attention_rule_bf16(const AttnRuleArgs& g, bool bwd, hipStream_t st);
 hipError_t attention_rule_f32(const AttnRuleArgs& g, bool bwd, hipStream_t st);
-hipError_t attention_rule_delta(int dt, const AttnRuleArgs& g, hipStream_t st);
 
 // ---- GELU with an 8-bit checkpoint of its input (format: gelu8.hip); rows of F % 4 == 0 values; dh may be dg, g may be null
 hipError_t gelu8_fwd(int dt, const void* h, void* g, int8_t* codes, uint8_t* exps, int64_t rows, int F, hipStream_t st);

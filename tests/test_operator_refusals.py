@@ -90,8 +90,8 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
         lambda: binding.attention_forward(q.half(), k.half(), k.half()),
         lambda: binding.attention_forward(q.transpose(2, 3), k, k),
         lambda: binding.AttentionRule(order="sideways"),
-        lambda: binding.AttentionRule(documents=torch.zeros(2, 10)),
-        lambda: binding.AttentionRule(documents=torch.zeros(10, 2, dtype=torch.int32).T),
+        lambda: binding.AttentionRule(documents=torch.zeros(2, 10)).describe(q, k),
+        lambda: binding.AttentionRule(documents=torch.zeros(10, 2, dtype=torch.int32).T).describe(q, k),
         lambda: binding.AttentionRule(documents=torch.zeros(2, 9, dtype=torch.int32)).describe(q, k),
         lambda: binding.AttentionRule(q_documents=torch.zeros(2, 10, dtype=torch.int32)).describe(q, k),
         lambda: binding.AttentionRule(order="prefix").describe(q, k),
