@@ -70,6 +70,8 @@ enum { PT_SGDM = 0, PT_ADAMW = 1 };
  * Sec. 4.1); BERT = per-token start / end logits (span QA, Sec. 4.1).  CLS (BERT only): the first
  * token's final activation -> linear classifier over n_out classes (sequence classification). */
 enum { PT_HEAD_DEFAULT = 0, PT_HEAD_CLS = 1 };
+/* Which keys a query's position lets it see: all; those up to its own; those, and the sample's first prefix[sample]. */
+enum { PT_ATTN_FULL = 0, PT_ATTN_CAUSAL = 1, PT_ATTN_PREFIX = 2 };
 
 typedef struct {
   int32_t arch;        /* PT_VIT_PRELN | PT_BERT_POSTLN                              */
@@ -90,6 +92,10 @@ typedef struct {
                           frozen layer does not need (Sec. 3.2.1 item 2) is planned for them: the state arena holds
                           gradients and moments of the tensors from block k_min on only, and the work arena no
                           saved activations of theirs                                                */
+  int32_t act8;        /* 1: active blocks keep their GELU's input as an 8-bit checkpoint (pt_gelu8_fwd) instead of the
+                          activation and its derivative: 1 F bytes a token and block in place of 4 F in PT_BF16 mode.  The
+                          backward pass takes both from the checkpoint, so gradients carry its rounding; the loss does
+                          not.  The top block under a first-token head keeps its few rows as ever           */
   int64_t cache_slots; /* 0 = no cache; slot i belongs to sample id i                */
   int64_t host_slots;  /* rows of the host tier: sample ids cache_slots .. cache_slots+host_slots-1 (0 = none) */
   int64_t window_slots;/* device rows the host tier is staged through, >= 2 B when host_slots > 0; they are
@@ -129,6 +135,24 @@ PT_API pt_status pt_destroy(pt_ctx* ctx);
  * on their next use (Sec. 3.4). */
 PT_API pt_status pt_set_freeze_boundary(pt_ctx* ctx, int32_t k);
 PT_API pt_status pt_get_freeze_boundary(const pt_ctx* ctx, int32_t* k /*HOST out*/);
+
+/* Attention under a rule (the formulas stand at pt_attention_fwd below) for every block of this context, from the next
+ * pt_frozen_forward on; rule NULL: plain attention again.  For padded batches, packed rows and prefix or causal models.
+ * The arrays are copied on the context's stream: slopes for good, documents and prefix lengths for batches whose sample
+ * b they describe in row b (the caller sets them again for a batch with others; a batch of more than n samples is
+ * PT_EINVAL).  Cached rows are those of the rule that they were written under: the caller keeps it the same per sample.
+ * Padding (documents below 0) takes no part in attention; the span head leaves it out of the softmax over the sequence,
+ * and a label on it has loss 0 and no gradient.  Everything else (positions, LayerNorm, MLP) is per token and unchanged.
+ * PT_ESTATE between pt_frozen_forward and pt_active_fwd_bwd of a batch. */
+typedef struct {
+  int32_t order;              /* PT_ATTN_*                                     */
+  int32_t n;                  /* samples that documents and prefix describe    */
+  float cap;                  /* 0: none                                       */
+  const float* slopes;        /* DEVICE [H] or NULL                            */
+  const int32_t* documents;   /* DEVICE [n,S] or NULL                          */
+  const int32_t* prefix;      /* DEVICE [n], PT_ATTN_PREFIX only               */
+} pt_attention_rule;
+PT_API pt_status pt_set_attention(pt_ctx* ctx, const pt_attention_rule* rule /*HOST, may be NULL*/);
 
 /* F_frozen for one batch of nb <= B samples.
  *  d_input    DEVICE. ViT: fp32 images [nb,chans,img,img]; BERT: int32 ids [nb,S].
@@ -336,7 +360,6 @@ PT_API pt_status pt_profile_read(pt_ctx* ctx, int32_t category, double* total_ms
  *   dtype PT_BF16: products of bf16 on the matrix cores, everything else fp32,
  * the probabilities and dS rounded to bf16 for the second products.  PT_F32: all
  * in fp32.  Sums are in a fixed order: results do not vary from run to run. */
-enum { PT_ATTN_FULL = 0, PT_ATTN_CAUSAL = 1, PT_ATTN_PREFIX = 2 };
 typedef struct {
   void* data;
   int64_t sample, row, head;   /* strides in elements */

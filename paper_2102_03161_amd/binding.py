@@ -32,7 +32,12 @@ class PtConfig(C.Structure):
                 ("F", C.c_int32), ("S", C.c_int32), ("B", C.c_int32), ("n_out", C.c_int32), ("img", C.c_int32),
                 ("patch", C.c_int32), ("chans", C.c_int32), ("vocab", C.c_int32), ("max_pos", C.c_int32),
                 ("ln_eps", C.c_float), ("optimizer", C.c_int32), ("head", C.c_int32), ("grad_accum", C.c_int32),
-                ("k_min", C.c_int32), ("cache_slots", C.c_int64), ("host_slots", C.c_int64), ("window_slots", C.c_int64)]
+                ("k_min", C.c_int32), ("act8", C.c_int32), ("cache_slots", C.c_int64), ("host_slots", C.c_int64), ("window_slots", C.c_int64)]
+
+
+class PtAttentionRule(C.Structure):
+    _fields_ = [("order", C.c_int32), ("n", C.c_int32), ("cap", C.c_float), ("slopes", C.c_void_p), ("documents", C.c_void_p),
+                ("prefix", C.c_void_p)]
 
 
 class PtOptHparams(C.Structure):
@@ -75,6 +80,7 @@ def load_library():
         "pt_destroy": [vp],
         "pt_set_freeze_boundary": [vp, i32],
         "pt_get_freeze_boundary": [vp, P(i32)],
+        "pt_set_attention": [vp, P(PtAttentionRule)],
         "pt_frozen_forward": [vp, vp, i32, P(i64), P(vp)],
         "pt_active_fwd_bwd": [vp, vp, vp, P(C.c_float)],
         "pt_last_loss": [vp, P(C.c_float)],
@@ -120,7 +126,7 @@ def load_library():
 
 
 def make_config(w: dict, B: int | None = None, cache_slots: int = 0, grad_accum: bool = False,
-                host_slots: int = 0, window_slots: int = 0, k_min: int = 0) -> PtConfig:
+                host_slots: int = 0, window_slots: int = 0, k_min: int = 0, act8: bool = False) -> PtConfig:
     """pt_config from a workload dict (see synth.WORKLOADS)."""
     return PtConfig(
         arch=PT_VIT_PRELN if w["arch"] == "vit" else PT_BERT_POSTLN,
@@ -129,7 +135,7 @@ def make_config(w: dict, B: int | None = None, cache_slots: int = 0, grad_accum:
         img=w["img"], patch=w["patch"], chans=w["chans"], vocab=w["vocab"], max_pos=w["max_pos"],
         ln_eps=w["ln_eps"], optimizer=PT_ADAMW if w["optimizer"] == "adamw" else PT_SGDM,
         head=PT_HEAD_CLS if w.get("head", "default") == "cls" else PT_HEAD_DEFAULT, grad_accum=1 if grad_accum else 0,
-        k_min=k_min, cache_slots=cache_slots, host_slots=host_slots, window_slots=window_slots)
+        k_min=k_min, act8=1 if act8 else 0, cache_slots=cache_slots, host_slots=host_slots, window_slots=window_slots)
 
 
 def query_arena_bytes(cfg: PtConfig):
@@ -388,6 +394,31 @@ class Context:
         k = C.c_int32()
         self._chk(self.lib.pt_get_freeze_boundary(self.h, C.byref(k)))
         return k.value
+
+    def set_attention(self, rule: AttentionRule | None):
+        """Attention of every block under `rule` (its scale and q0 are the context's own: 1 / sqrt(D / H) and 0), from the next
+        batch on; None: plain attention.  documents [n, S] and prefix [n] describe the batches' samples by position."""
+        if rule is None:
+            self._chk(self.lib.pt_set_attention(self.h, None))
+            return
+        if rule.scale is not None or rule.q0 != 0 or rule.q_documents is not rule.documents:
+            _refuse("a context's rule has neither scale nor q0, and one set of documents")
+        if not _DTYPES:
+            _op_setup()
+        r = PtAttentionRule(ATTN_ORDERS[rule.order], 0, rule.cap)
+        given = [t for t in (rule.documents, rule.prefix if rule.order == "prefix" else None) if t is not None]
+        if given:
+            r.n = given[0].shape[0]
+        if rule.slopes is not None:
+            r.slopes = _plain(rule.slopes, _torch.float32, (self.cfg.H,), "slopes")
+        if rule.documents is not None:
+            r.documents = _plain(rule.documents, _torch.int32, (r.n, self.cfg.S), "documents")
+        if rule.order == "prefix" and rule.prefix is not None:
+            r.prefix = _plain(rule.prefix, _torch.int32, (r.n,), "prefix")
+        for t in (rule.slopes, *given):
+            if t is not None and t.device != self.arenas[0].device:
+                _refuse(f"a tensor on {t.device}, the context on {self.arenas[0].device}")
+        self._chk(self.lib.pt_set_attention(self.h, r))
 
     def frozen_forward(self, d_input, sample_ids=None) -> int:
         """d_input: torch tensor on the device.  Returns the device pointer of h_k."""

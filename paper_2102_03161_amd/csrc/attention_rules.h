@@ -28,8 +28,8 @@ struct RuleRows {
   int prefix;
   __device__ __forceinline__ RuleRows(const AttnRuleArgs& g, int b) {
     const int64_t r = g.bmap ? g.bmap[b] : b;
-    q = g.qdoc ? g.qdoc + r * g.Sq : nullptr;
-    k = g.kdoc ? g.kdoc + r * g.Sk : nullptr;
+    q = g.qdoc ? g.qdoc + r * g.qdoc_ld : nullptr;
+    k = g.kdoc ? g.kdoc + r * g.kdoc_ld : nullptr;
     prefix = g.order == 2 ? g.prefix[r] : 0;
   }
   __device__ __forceinline__ int lim(const AttnRuleArgs& g, int i) const {

@@ -70,6 +70,7 @@ struct AttnRuleArgs {
   const int32_t* qdoc;       // [*, Sq] or null; below 0: padding
   const int32_t* kdoc;       // [*, Sk] or null
   const int32_t* prefix;     // [*], order 2
+  int64_t qdoc_ld, kdoc_ld;  // elements between the documents of successive samples
   const int64_t* bmap;       // sample b's documents and prefix are those of row bmap[b]; null: b
   HeadView q, k, v, o, d_o, dq, dk, dv;
   float* lse; int64_t lse_b, lse_h;   // forward: written unless null; backward: read
@@ -136,8 +137,9 @@ void bert_embed_bwd(const int32_t* ids, const float* demb, float* dEw, float* dE
 void ce_rows(int dt, const float* z, const int32_t* labels, float* loss_rows, void* dz, int nb, int C, hipStream_t st);
 // BERT QA: x [nb,S,D] (T), W [D,2], b[2] (T).  z fp32 [nb,S,2] -> CE over S per column.
 void qa_logits(int dt, const void* x, const void* W, const void* b, float* z, int rows, int D, hipStream_t st);
-void qa_ce(int dt, const float* z, const int32_t* labels, float* loss_rows /*[nb]*/, float* dz /*fp32 [nb,S,2]*/, int nb,
-           int S, hipStream_t st);
+// docs (may be null): [nb,S], tokens with a document below 0 are padding and no candidates; a label there counts nothing
+void qa_ce(int dt, const float* z, const int32_t* labels, const int32_t* docs, float* loss_rows /*[nb]*/, float* dz /*fp32 [nb,S,2]*/,
+           int nb, int S, hipStream_t st);
 // dx[t] = dz[t,0] W[:,0] + dz[t,1] W[:,1]; dW[d,c] = sum_t x[t,d] dz[t,c]; db[c] = sum_t dz[t,c]
 size_t qa_partial_floats(int D);
 void qa_head_bwd(int dt, const void* x, const void* W, const float* dz, float* dx, float* dW, float* db, float* partial,

@@ -66,6 +66,7 @@ AttnRuleArgs rule_args(const pt_attention* a) {
   g.nb = a->nb; g.Sq = a->Sq; g.Sk = a->Sk; g.H = a->H; g.Hkv = a->Hkv; g.dh = a->dh;
   g.order = a->order; g.q0 = a->q0; g.scale = a->scale; g.cap = a->cap; g.slopes = a->slopes;
   g.qdoc = a->q_documents; g.kdoc = a->k_documents; g.prefix = a->prefix;
+  g.qdoc_ld = a->Sq; g.kdoc_ld = a->Sk;
   g.lse_h = a->Sq; g.lse_b = (int64_t)a->H * a->Sq;
   return g;
 }

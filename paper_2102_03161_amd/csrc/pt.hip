@@ -44,6 +44,7 @@ enum BlockTensor { LN1_G, LN1_B, WQKV, BQKV, WO, BO, LN2_G, LN2_B, W1, B1, W2, B
 // byte offsets into the work arena of the tensors one block keeps
 struct Slot {
   size_t U, QKV, CTX, Y, WN, HP, G, LSE, MU1, RS1, MU2, RS2;   // HP: GELU'(pre-activation), G: GELU(pre-activation)
+  size_t C8, E8;   // act8: codes and exponents of the pre-activation in place of HP; G is one buffer that all blocks use
 };
 
 struct Plan {
@@ -59,6 +60,7 @@ struct Plan {
   size_t HKOUT, sA, sB, sC, sD, oA, oB, oC, oD, oE, oE2, dF, dQKV, DELTA;
   // dense copies of the first token's rows (top block's backward under a first-token head)
   size_t rG, rHP, rDF, rXa, rXb, rCTX, rDO, rOC, rOD, rDCTX, rS0, rS1, rS2, rST;  // s*: fp32 gradient stream, o*: T operand copies
+  size_t DOCS, PREFIX, SLOPES;  // the attention rule's arrays (pt_set_attention)
   size_t PATCH, EMB, DEMB, MUE, RSE, CHAINWS, IDS;  // front ends (EMB: ViT patch embeddings / BERT embedding sum; IDS: the batch's token ids)
   size_t CFEAT, MUF, RSF, LOGITS, DZ, DC, LOSSROWS;  // heads
   int ln_slots = 1;
@@ -90,6 +92,7 @@ bool validate(const pt_config& c, std::string* why) {
   if (c.host_slots == 0 && c.window_slots != 0) return bad("window_slots without host_slots");
   if (!(c.ln_eps >= 0.f)) return bad("ln_eps");
   if (c.k_min < 0 || c.k_min > c.L) return bad("k_min outside 0..L");
+  if (c.act8 != 0 && c.act8 != 1) return bad("act8 is 0 or 1");
   if ((int64_t)c.B * c.S > (1 << 24)) return bad("B*S too large");
   // sequence length: the supported range of the fp32 kernels; the first-token kernels keep a score row of the sequence in LDS
   constexpr size_t kLdsPerCu = 160 * 1024;
@@ -162,12 +165,20 @@ void make_plan(const pt_config& c, Plan* p) {
     for (int l = 0; l <= L; ++l) p->X[l] = l < c.k_min ? ping[l & 1] : take(TD);
   }
   p->slot.resize(L + 1);
+  const size_t g8 = c.act8 ? take(TF) : 0;   // GELU(pre-activation) of the block that is being computed
   for (int l = c.k_min < L ? c.k_min : L; l <= L; ++l) {
     Slot& s = p->slot[l];
     // post-LN keeps the two pre-LayerNorm sums (U, WN) in fp32
     const size_t TDsum = c.arch == PT_BERT_POSTLN ? T * D * 4 : TD;
     s.U = take(TDsum); s.QKV = take(3 * TD); s.CTX = take(TD); s.Y = take(TD); s.WN = take(TDsum);
-    s.HP = take(TF); s.G = take(TF); s.LSE = take(BHS);
+    s.C8 = s.E8 = 0;
+    if (c.act8) {
+      s.HP = 0; s.G = g8;
+      if (l < L) { s.C8 = take(T * F); s.E8 = take(T * ((F + 31) / 32)); }
+    } else {
+      s.HP = take(TF); s.G = take(TF);
+    }
+    s.LSE = take(BHS);
     s.MU1 = take(T * 4); s.RS1 = take(T * 4); s.MU2 = take(T * 4); s.RS2 = take(T * 4);
   }
   for (int l = 0; l < c.k_min && l < L; ++l) p->slot[l] = p->slot[L];   // never used: these blocks take the prefix's scratch slot
@@ -201,6 +212,7 @@ void make_plan(const pt_config& c, Plan* p) {
     if (c.head == PT_HEAD_CLS) { p->LOGITS = take((size_t)B * c.n_out * 4); p->DZ = take((size_t)B * c.n_out * e); }
     else { p->LOGITS = take(T * 2 * 4); p->DZ = take(T * 2 * 4); }
   }
+  p->DOCS = take(T * 4); p->PREFIX = take((size_t)B * 4); p->SLOPES = take((size_t)c.H * 4);
   p->LOSSROWS = take((size_t)B * 4);
   p->LOSS = take(4);
   p->LOSSACC = take(4);
@@ -265,6 +277,9 @@ struct pt_ctx {
   int phase = 0;  // 0 idle, 1 frozen forward done, 2 backward done
   int nb = 0;
   void* last_hk = nullptr;
+  struct { bool on = false, slopes = false, docs = false, prefix = false; int order = 0, n = 0; float cap = 0.f; } rule;   // pt_set_attention
+  const int64_t* rule_map = nullptr;   // device: sample of the caller's batch that position b of the blocks' batch is; null: b
+  hipError_t op_err = hipSuccess;      // first failed launch of an operator since the last check
   void* last_dhk = nullptr;
   std::vector<int32_t> slot_k;  // boundary a cache row was written at, -1 = empty (HBM rows, then host rows)
   // host tier: rows of sample ids >= cache_slots live in pinned host memory and pass through a window of
@@ -430,6 +445,70 @@ pt_status flush_deferred_norms(pt_ctx* c);   // norms begun but not enqueued yet
     if (e_ != hipSuccess) return fail(ctx, PT_EDEVICE, std::string(#expr) + ": " + hipGetErrorString(e_)); \
   } while (0)
 
+void ctx_gelu8(pt_ctx* c, hipError_t e) {
+  if (c->op_err == hipSuccess) c->op_err = e;
+}
+
+// The context's attention over packed qkv, plain or under the rule of pt_set_attention.  first: only each sample's first query
+// (rows of ctx and do dense, dqkv written whole).
+AttnRuleArgs rule_args(pt_ctx* c, const void* qkv, int ns, bool first) {
+  const pt_config& cf = c->cfg;
+  const int S = cf.S, D = cf.D, H = cf.H, dh = D / H;
+  const Plan& p = c->plan;
+  AttnRuleArgs a{};
+  a.nb = ns; a.Sq = first ? 1 : S; a.Sk = S; a.H = a.Hkv = H; a.dh = dh;
+  a.order = c->rule.order; a.cap = c->rule.cap; a.scale = 1.f / std::sqrt((float)dh);
+  a.slopes = c->rule.slopes ? c->wf(p.SLOPES) : nullptr;
+  a.qdoc = a.kdoc = c->rule.docs ? reinterpret_cast<const int32_t*>(c->w(p.DOCS)) : nullptr;
+  a.qdoc_ld = a.kdoc_ld = S;
+  a.prefix = c->rule.prefix ? reinterpret_cast<const int32_t*>(c->w(p.PREFIX)) : nullptr;
+  a.bmap = c->rule_map;
+  const char* q = static_cast<const char*>(qkv);
+  const int64_t row = 3 * (int64_t)D;
+  a.q = HeadView{q, S * row, row, dh};
+  a.k = HeadView{q + D * c->esz, S * row, row, dh};
+  a.v = HeadView{q + 2 * D * c->esz, S * row, row, dh};
+  a.lse_h = S; a.lse_b = (int64_t)H * S;
+  return a;
+}
+void ctx_attention_fwd(pt_ctx* c, const void* qkv, void* ctx, float* lse, int ns, bool first) {
+  const pt_config& cf = c->cfg;
+  const int dh = cf.D / cf.H;
+  if (!c->rule.on) {
+    if (first) attention_fwd_first_query(c->dt, qkv, ctx, lse, ns, cf.S, cf.H, dh, c->st);
+    else attention_fwd(c->dt, qkv, ctx, lse, ns, cf.S, cf.H, dh, c->st);
+    return;
+  }
+  AttnRuleArgs a = rule_args(c, qkv, ns, first);
+  a.o = HeadView{ctx, (first ? 1 : (int64_t)cf.S) * cf.D, cf.D, dh};
+  a.lse = lse;
+  const hipError_t e = attention_rule_fwd(c->dt, a, c->st);
+  if (c->op_err == hipSuccess) c->op_err = e;
+}
+void ctx_attention_bwd(pt_ctx* c, const void* qkv, const void* ctx, const void* dctx, const float* lse, void* dqkv, int ns, bool first) {
+  const pt_config& cf = c->cfg;
+  const int dh = cf.D / cf.H;
+  float* delta = c->wf(c->plan.DELTA);
+  if (!c->rule.on) {
+    if (first) attention_bwd_first_query(c->dt, qkv, ctx, dctx, lse, dqkv, ns, cf.S, cf.H, dh, c->st);
+    else attention_bwd(c->dt, qkv, ctx, dctx, lse, dqkv, delta, ns, cf.S, cf.H, dh, c->st);
+    return;
+  }
+  AttnRuleArgs a = rule_args(c, qkv, ns, first);
+  const int64_t out = (first ? 1 : (int64_t)cf.S) * cf.D;
+  a.o = HeadView{ctx, out, cf.D, dh};
+  a.d_o = HeadView{dctx, out, cf.D, dh};
+  char* d = static_cast<char*>(dqkv);
+  a.dq = HeadView{d, a.q.b, a.q.t, dh};
+  a.dk = HeadView{d + cf.D * c->esz, a.q.b, a.q.t, dh};
+  a.dv = HeadView{d + 2 * cf.D * c->esz, a.q.b, a.q.t, dh};
+  a.lse = const_cast<float*>(lse);
+  a.delta = delta;
+  if (first) fill_zero(dqkv, (size_t)ns * a.q.b * c->esz, c->st);   // dq of the other queries
+  const hipError_t e = attention_rule_bwd(c->dt, a, c->st);
+  if (c->op_err == hipSuccess) c->op_err = e;
+}
+
 // ---------------------------------------------------------------------------
 // one encoder block, forward.  save == false: forward-only (nothing kept).
 // ---------------------------------------------------------------------------
@@ -447,21 +526,31 @@ void block_forward(pt_ctx* c, int l, const void* xin, void* xout, const Slot& s,
     m.epi = epi; m.bias = c->cp(bid); m.aux = aux; m.aux_out = aux_out; m.ld_aux = N; m.c_f32 = out_f32;
     { ProfScope ps_(c, gemm_cat(dt, m), 2.0 * m.M * m.N * m.K); gemm(dt, m, st); }
   };
+  // first MLP product and GELU.  Under act8 the pre-activation itself is the product (into dF, which only the backward pass uses
+  // otherwise) and leaves as its 8-bit checkpoint.
+  auto up = [&](const void* in) {
+    if (save && g.act8) {
+      lin(in, D, c->blk(l, W1), c->blk(l, B1), c->w(c->plan.dF), F, EPI_BIAS, nullptr, nullptr);
+      ctx_gelu8(c, gelu8_fwd(dt, c->w(c->plan.dF), c->w(s.G), reinterpret_cast<int8_t*>(c->w(s.C8)), reinterpret_cast<uint8_t*>(c->w(s.E8)), Tn, F, st));
+    } else {
+      lin(in, D, c->blk(l, W1), c->blk(l, B1), c->w(s.G), F, EPI_BIAS_GELU, nullptr, save ? c->w(s.HP) : nullptr);
+    }
+  };
   if (g.arch == PT_VIT_PRELN) {
     { prof_ln_fwd(c, dt, false, xin, D, c->cp(c->blk(l, LN1_G)), c->cp(c->blk(l, LN1_B)), c->w(s.U), D, mu1, rs1, Tn, D, g.ln_eps, st); }
     lin(c->w(s.U), D, c->blk(l, WQKV), c->blk(l, BQKV), c->w(s.QKV), 3 * D, EPI_BIAS, nullptr, nullptr);
-    { ProfScope ps_(c, PT_PROF_ATTN_FWD, 4.0 * ns * g.H * (double)g.S * g.S * (D / g.H)); attention_fwd(dt, c->w(s.QKV), c->w(s.CTX), lse, ns, g.S, g.H, D / g.H, st); }
+    { ProfScope ps_(c, PT_PROF_ATTN_FWD, 4.0 * ns * g.H * (double)g.S * g.S * (D / g.H)); ctx_attention_fwd(c, c->w(s.QKV), c->w(s.CTX), lse, ns, false); }
     lin(c->w(s.CTX), D, c->blk(l, WO), c->blk(l, BO), c->w(s.Y), D, EPI_BIAS_RES, xin, nullptr);
     { prof_ln_fwd(c, dt, false, c->w(s.Y), D, c->cp(c->blk(l, LN2_G)), c->cp(c->blk(l, LN2_B)), c->w(s.WN), D, mu2, rs2, Tn, D, g.ln_eps, st); }
-    lin(c->w(s.WN), D, c->blk(l, W1), c->blk(l, B1), c->w(s.G), F, EPI_BIAS_GELU, nullptr, save ? c->w(s.HP) : nullptr);
+    up(c->w(s.WN));
     lin(c->w(s.G), F, c->blk(l, W2), c->blk(l, B2), xout, D, EPI_BIAS_RES, c->w(s.Y), nullptr);
   } else {
     // post-LN: U holds x + Attn(x) in fp32, Y = LN1(U), WN holds Y + MLP(Y) in fp32, out = LN2(WN)
     lin(xin, D, c->blk(l, WQKV), c->blk(l, BQKV), c->w(s.QKV), 3 * D, EPI_BIAS, nullptr, nullptr);
-    { ProfScope ps_(c, PT_PROF_ATTN_FWD, 4.0 * ns * g.H * (double)g.S * g.S * (D / g.H)); attention_fwd(dt, c->w(s.QKV), c->w(s.CTX), lse, ns, g.S, g.H, D / g.H, st); }
+    { ProfScope ps_(c, PT_PROF_ATTN_FWD, 4.0 * ns * g.H * (double)g.S * g.S * (D / g.H)); ctx_attention_fwd(c, c->w(s.QKV), c->w(s.CTX), lse, ns, false); }
     lin(c->w(s.CTX), D, c->blk(l, WO), c->blk(l, BO), c->w(s.U), D, EPI_BIAS_RES, xin, nullptr, true);
     { prof_ln_fwd(c, dt, true, c->w(s.U), D, c->cp(c->blk(l, LN1_G)), c->cp(c->blk(l, LN1_B)), c->w(s.Y), D, mu1, rs1, Tn, D, g.ln_eps, st); }
-    lin(c->w(s.Y), D, c->blk(l, W1), c->blk(l, B1), c->w(s.G), F, EPI_BIAS_GELU, nullptr, save ? c->w(s.HP) : nullptr);
+    up(c->w(s.Y));
     lin(c->w(s.G), F, c->blk(l, W2), c->blk(l, B2), c->w(s.WN), D, EPI_BIAS_RES, c->w(s.Y), nullptr, true);
     { prof_ln_fwd(c, dt, true, c->w(s.WN), D, c->cp(c->blk(l, LN2_G)), c->cp(c->blk(l, LN2_B)), xout, D, mu2, rs2, Tn, D, g.ln_eps, st); }
   }
@@ -540,17 +629,25 @@ void block_backward(pt_ctx* c, int l, const void* xin, const Slot& s, GradBufs d
     m.M = Tn; m.N = Kin; m.K = Nout; m.epi = epi; m.aux = aux; m.ld_aux = Kin; m.c_f32 = out_f32;
     { ProfScope ps_(c, gemm_cat(dt, m), 2.0 * m.M * m.N * m.K); gemm(dt, m, st); }
   };
+  // dF = gradient of the pre-activation.  Under act8 GELU' comes from the 8-bit checkpoint, and with it the activation that W2's
+  // weight gradient reads (in the buffer that all blocks use: the gradients of the block above, if they were held back, are
+  // launched before this).
+  auto down = [&](const void* dY) {
+    dgrad(dY, D, c->blk(l, W2), dF, F, g.act8 ? EPI_STORE : EPI_MUL_DGELU, g.act8 ? nullptr : c->w(s.HP), false);
+    if (g.act8)
+      ctx_gelu8(c, gelu8_bwd(dt, reinterpret_cast<const int8_t*>(c->w(s.C8)), reinterpret_cast<const uint8_t*>(c->w(s.E8)), dF, dF, c->w(s.G), Tn, F, st));
+  };
   if (g.arch == PT_VIT_PRELN) {
     // the gradient of b2 (column sums of dout) came with the kernel that produced dout
     wgrad(c->w(s.G), F, dout.o, D, c->blk(l, W2), -1);
-    dgrad(dout.o, D, c->blk(l, W2), dF, F, EPI_MUL_DGELU, c->w(s.HP), false);
+    down(dout.o);
     wgrad(c->w(s.WN), D, dF, F, c->blk(l, W1), c->blk(l, B1));
     dgrad(dF, F, c->blk(l, W1), oC, D, EPI_STORE, nullptr, false);                      // oC = dL/dLN2out
     { prof_ln_bwd(c, dt, false, false, oC, D, c->w(s.Y), D, c->wf(s.MU2), c->wf(s.RS2), c->cp(c->blk(l, LN2_G)), dout.s, D, sC, oD,
                   D, c->gp(c->blk(l, LN2_G)), c->gp(c->blk(l, LN2_B)), c->gp(c->blk(l, BO)), Tn, D, st); }  // sC / oD = dL/dY
     wgrad(c->w(s.CTX), D, oD, D, c->blk(l, WO), -1);
     dgrad(oD, D, c->blk(l, WO), oC, D, EPI_STORE, nullptr, false);                      // oC = dL/dCTX
-    { ProfScope ps_(c, PT_PROF_ATTN_BWD, 8.0 * ns * g.H * (double)g.S * g.S * (D / g.H)); attention_bwd(dt, c->w(s.QKV), c->w(s.CTX), oC, c->wf(s.LSE), dQKV, c->wf(p.DELTA), ns, g.S, g.H, D / g.H, st); }
+    { ProfScope ps_(c, PT_PROF_ATTN_BWD, 8.0 * ns * g.H * (double)g.S * g.S * (D / g.H)); ctx_attention_bwd(c, c->w(s.QKV), c->w(s.CTX), oC, c->wf(s.LSE), dQKV, ns, false); }
     wgrad(c->w(s.U), D, dQKV, 3 * D, c->blk(l, WQKV), c->blk(l, BQKV));
     dgrad(dQKV, 3 * D, c->blk(l, WQKV), oC, D, EPI_STORE, nullptr, false);              // oC = dL/dU
     // The block's last LayerNorm backward pass (-> dx) and its weight gradients do not depend on each other:
@@ -590,14 +687,14 @@ void block_backward(pt_ctx* c, int l, const void* xin, const Slot& s, GradBufs d
     { prof_ln_bwd(c, dt, true, true, dout.s, D, c->w(s.WN), D, c->wf(s.MU2), c->wf(s.RS2), c->cp(c->blk(l, LN2_G)), nullptr, 0, sC,
                   oE, D, c->gp(c->blk(l, LN2_G)), c->gp(c->blk(l, LN2_B)), c->gp(c->blk(l, B2)), Tn, D, st); }  // sC / oE = dL/d(Y+MLP)
     wgrad(c->w(s.G), F, oE, D, c->blk(l, W2), -1);
-    dgrad(oE, D, c->blk(l, W2), dF, F, EPI_MUL_DGELU, c->w(s.HP), false);
+    down(oE);
     wgrad(c->w(s.Y), D, dF, F, c->blk(l, W1), c->blk(l, B1));
     dgrad(dF, F, c->blk(l, W1), sD, D, EPI_RES, sC, true);                              // sD = dL/dY
     { prof_ln_bwd(c, dt, true, true, sD, D, c->w(s.U), D, c->wf(s.MU1), c->wf(s.RS1), c->cp(c->blk(l, LN1_G)), nullptr, 0, sC, oC,
                   D, c->gp(c->blk(l, LN1_G)), c->gp(c->blk(l, LN1_B)), c->gp(c->blk(l, BO)), Tn, D, st); }  // sC / oC = dL/d(x+Attn)
     wgrad(c->w(s.CTX), D, oC, D, c->blk(l, WO), -1);
     dgrad(oC, D, c->blk(l, WO), oD, D, EPI_STORE, nullptr, false);                      // oD = dL/dCTX
-    { ProfScope ps_(c, PT_PROF_ATTN_BWD, 8.0 * ns * g.H * (double)g.S * g.S * (D / g.H)); attention_bwd(dt, c->w(s.QKV), c->w(s.CTX), oD, c->wf(s.LSE), dQKV, c->wf(p.DELTA), ns, g.S, g.H, D / g.H, st); }
+    { ProfScope ps_(c, PT_PROF_ATTN_BWD, 8.0 * ns * g.H * (double)g.S * g.S * (D / g.H)); ctx_attention_bwd(c, c->w(s.QKV), c->w(s.CTX), oD, c->wf(s.LSE), dQKV, ns, false); }
     wgrad(xin, D, dQKV, 3 * D, c->blk(l, WQKV), c->blk(l, BQKV));
     if (need_dx) dgrad(dQKV, 3 * D, c->blk(l, WQKV), dx.s, D, EPI_RES, sC, true);
     if (dt != 0) {   // held back for the next block's first LayerNorm pass (or the end of the sweep)
@@ -637,7 +734,7 @@ void block_forward_first_rows(pt_ctx* c, int l, const void* xin, void* xout, con
   };
   auto attn = [&]() {
     ProfScope ps_(c, PT_PROF_ATTN_FWD, 4.0 * ns * g.H * (double)g.S * (D / g.H));
-    attention_fwd_first_query(dt, c->w(s.QKV), rCTX, c->wf(s.LSE), ns, g.S, g.H, D / g.H, st);
+    ctx_attention_fwd(c, c->w(s.QKV), rCTX, c->wf(s.LSE), ns, true);
   };
   if (g.arch == PT_VIT_PRELN) {
     { prof_ln_fwd(c, dt, false, xin, D, c->cp(c->blk(l, LN1_G)), c->cp(c->blk(l, LN1_B)), c->w(s.U), D, c->wf(s.MU1), c->wf(s.RS1), Tn, D, g.ln_eps, st); }
@@ -734,7 +831,7 @@ void block_backward_first_rows(pt_ctx* c, int l, const void* xin, const Slot& s,
     wgrad_rows(rCTX, D, rOD, D, c->blk(l, WO), -1);
     wgrad_rows_launch();
     dgrad(rOD, D, c->blk(l, WO), rDCTX, D, EPI_STORE, nullptr, false, ns);                // dL/dCTX
-    { ProfScope ps_(c, PT_PROF_ATTN_BWD, 8.0 * ns * g.H * (double)g.S * (D / g.H)); attention_bwd_first_query(dt, c->w(s.QKV), rCTX, rDCTX, c->wf(s.LSE), dQKV, ns, g.S, g.H, D / g.H, st); }
+    { ProfScope ps_(c, PT_PROF_ATTN_BWD, 8.0 * ns * g.H * (double)g.S * (D / g.H)); ctx_attention_bwd(c, c->w(s.QKV), rCTX, rDCTX, c->wf(s.LSE), dQKV, ns, true); }
     wgrad(c->w(s.U), D, dQKV, 3 * D, c->blk(l, WQKV), c->blk(l, BQKV), Tn);
     dgrad(dQKV, 3 * D, c->blk(l, WQKV), oC, D, EPI_STORE, nullptr, false, Tn);            // dL/dU
     // dL/dY (rS1), the residual branch of dL/dx, is non-zero in the first tokens' rows only: it is added to
@@ -761,7 +858,7 @@ void block_backward_first_rows(pt_ctx* c, int l, const void* xin, const Slot& s,
     dgrad(rOC, D, c->blk(l, WO), rDCTX, D, EPI_STORE, nullptr, false, ns);                // dL/dCTX
     const RowCopy out[] = {back(rS1, D, 4, dout.s, SD)};
     strided_rows_copy(out, 1, ns, st);
-    { ProfScope ps_(c, PT_PROF_ATTN_BWD, 8.0 * ns * g.H * (double)g.S * (D / g.H)); attention_bwd_first_query(dt, c->w(s.QKV), rCTX, rDCTX, c->wf(s.LSE), dQKV, ns, g.S, g.H, D / g.H, st); }
+    { ProfScope ps_(c, PT_PROF_ATTN_BWD, 8.0 * ns * g.H * (double)g.S * (D / g.H)); ctx_attention_bwd(c, c->w(s.QKV), rCTX, rDCTX, c->wf(s.LSE), dQKV, ns, true); }
     wgrad(xin, D, dQKV, 3 * D, c->blk(l, WQKV), c->blk(l, BQKV), Tn);
     if (need_dx) dgrad(dQKV, 3 * D, c->blk(l, WQKV), dx.s, D, EPI_RES, dout.s, true, Tn);
   }
@@ -811,6 +908,12 @@ void front_backward(pt_ctx* c, const float* dx, int ns) {
     bert_embed_bwd(reinterpret_cast<const int32_t*>(c->w(p.IDS)), c->wf(p.DEMB), c->gp(0), c->gp(1),
                    reinterpret_cast<int32_t*>(c->w(p.CHAINWS)), ns, g.S, D, g.vocab, st);
   }
+}
+
+hipError_t take_op_err(pt_ctx* c) {
+  const hipError_t e = c->op_err;
+  c->op_err = hipSuccess;
+  return e;
 }
 
 // stage `n` int64 values for the device; returns the device pointer
@@ -969,6 +1072,30 @@ pt_status pt_set_freeze_boundary(pt_ctx* c, int32_t k) {
   return PT_OK;
 }
 
+pt_status pt_set_attention(pt_ctx* c, const pt_attention_rule* r) {
+  if (!c) return PT_EINVAL;
+  if (c->phase == 1) return fail(c, PT_ESTATE, "the attention rule cannot change between a batch's forward and backward pass");
+  if (!r) { c->rule = {}; return PT_OK; }
+  const pt_config& g = c->cfg;
+  const Plan& p = c->plan;
+  if (r->order != PT_ATTN_FULL && r->order != PT_ATTN_CAUSAL && r->order != PT_ATTN_PREFIX) return fail(c, PT_EINVAL, "order");
+  if (!(r->cap >= 0.f) || !std::isfinite(r->cap * 3.f) || (r->cap > 0.f && !std::isfinite(3.f / r->cap))) return fail(c, PT_EINVAL, "cap must be 0 or a positive finite number");
+  if (r->order == PT_ATTN_PREFIX && !r->prefix) return fail(c, PT_EINVAL, "PT_ATTN_PREFIX needs prefix lengths");
+  if ((r->documents || r->prefix) && (r->n < 1 || r->n > g.B)) return fail(c, PT_EINVAL, "n outside 1..B");
+  if (g.S > kRuleMaxRows || 2 * (int64_t)g.B * g.H * ((g.S + 63) / 64) >= (1 << 24)) return fail(c, PT_EINVAL, "batch or sequence too long for attention under a rule");
+  if (r->documents) HIP_TRY(c, hipMemcpyAsync(c->w(p.DOCS), r->documents, (size_t)r->n * g.S * 4, hipMemcpyDeviceToDevice, c->st));
+  if (r->order == PT_ATTN_PREFIX) HIP_TRY(c, hipMemcpyAsync(c->w(p.PREFIX), r->prefix, (size_t)r->n * 4, hipMemcpyDeviceToDevice, c->st));
+  if (r->slopes) HIP_TRY(c, hipMemcpyAsync(c->w(p.SLOPES), r->slopes, (size_t)g.H * 4, hipMemcpyDeviceToDevice, c->st));
+  c->rule.on = true;
+  c->rule.order = r->order;
+  c->rule.cap = r->cap;
+  c->rule.n = r->n;
+  c->rule.slopes = r->slopes != nullptr;
+  c->rule.docs = r->documents != nullptr;
+  c->rule.prefix = r->order == PT_ATTN_PREFIX;
+  return PT_OK;
+}
+
 // ---- host tier of the activation cache (Sec. 3.4 / App. E: hierarchical cache with a sliding window) ----
 namespace {
 
@@ -1094,6 +1221,8 @@ pt_status pt_frozen_forward(pt_ctx* c, const void* d_input, int32_t nb, const in
   const pt_config& g = c->cfg;
   const Plan& p = c->plan;
   if (nb < 1 || nb > g.B) return fail(c, PT_EINVAL, "batch outside 1..B");
+  if ((c->rule.docs || c->rule.prefix) && nb > c->rule.n) return fail(c, PT_EINVAL, "the attention rule has documents or prefix lengths of fewer samples");
+  c->rule_map = nullptr;
   const int k = c->k;
   const size_t row_bytes = (size_t)g.S * g.D * c->esz;
   if (k == 0) {
@@ -1182,6 +1311,8 @@ pt_status pt_frozen_forward(pt_ctx* c, const void* d_input, int32_t nb, const in
       { prof_copy_rows(c, c->w(p.HKOUT), nullptr, c->cache, dsrc, nb, row_bytes, c->st); }
       c->last_hk = c->w(p.HKOUT);
     } else {
+      // the blocks below see the batch in sorted order: where the rule finds a sample's documents and prefix
+      if (!identity && (c->rule.docs || c->rule.prefix)) c->rule_map = stg.put(std::vector<int64_t>(order.begin(), order.end()), &cerr);
       if (n_miss > 0) {
         const int64_t* dmap = nullptr;
         if (!(identity && n_miss == nb)) {
@@ -1228,6 +1359,7 @@ pt_status pt_frozen_forward(pt_ctx* c, const void* d_input, int32_t nb, const in
         c->last_hk = c->w(p.HKOUT);
       }
     }
+    c->rule_map = nullptr;
     HIP_TRY(c, stg.end());
     if (cerr != hipSuccess) return fail(c, PT_EDEVICE, hipGetErrorString(cerr));
     if (host_used) {
@@ -1255,6 +1387,7 @@ pt_status pt_frozen_forward(pt_ctx* c, const void* d_input, int32_t nb, const in
         c->slot_k[(size_t)sample_ids[i]] = k;
       }
   }
+  HIP_TRY(c, take_op_err(c));
   HIP_TRY(c, hipGetLastError());
   c->nb = nb;
   c->phase = 1;
@@ -1369,7 +1502,7 @@ pt_status pt_active_fwd_bwd(pt_ctx* c, const void* d_hk, const int32_t* d_labels
   } else {
     const int hW = c->head(0), hbias = c->head(1);
     qa_logits(dt, x, c->cp(hW), c->cp(hbias), c->wf(p.LOGITS), nb * S, D, st);
-    qa_ce(dt, c->wf(p.LOGITS), d_labels, c->wf(p.LOSSROWS), c->wf(p.DZ), nb, S, st);
+    qa_ce(dt, c->wf(p.LOGITS), d_labels, c->rule.docs ? reinterpret_cast<const int32_t*>(c->w(p.DOCS)) : nullptr, c->wf(p.LOSSROWS), c->wf(p.DZ), nb, S, st);
     mean_reduce(c->wf(p.LOSSROWS), nb, c->wf(p.LOSS), st);
     qa_head_bwd(dt, x, c->cp(hW), c->wf(p.DZ), dcur.s, c->gp(hW), c->gp(hbias), c->wf(p.QAPART), nb * S, D, st);
   }
@@ -1389,6 +1522,7 @@ pt_status pt_active_fwd_bwd(pt_ctx* c, const void* d_hk, const int32_t* d_labels
   if (k == 0) front_backward(c, dcur.s, nb);
   flush_ln_reductions(c);
   c->last_dhk = dcur.s;
+  HIP_TRY(c, take_op_err(c));
   HIP_TRY(c, hipGetLastError());
   c->phase = 2;
   if (loss_out) return pt_last_loss(c, loss_out);

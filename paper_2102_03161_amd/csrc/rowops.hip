@@ -642,32 +642,36 @@ void qa_logits(int dt, const void* x, const void* W, const void* b, float* z, in
   else hipLaunchKernelGGL(qa_logits_kernel<bf16>, grid, dim3(256), 0, st, (const bf16*)x, (const bf16*)W, (const bf16*)b, z, rows, D);
 }
 
-// one workgroup per sample; cross-entropy over the sequence axis for each of the two logit columns
+// one workgroup per sample; cross-entropy over the sequence axis for each of the two logit columns.  Padding (docs below 0) is left
+// out of the axis; a label that is padding has loss 0 and no gradient.
 __global__ __launch_bounds__(256) void qa_ce_kernel(const float* __restrict__ z, const int32_t* __restrict__ labels,
-                                                    float* __restrict__ loss_rows, float* __restrict__ dz, int nb, int S) {
+                                                    const int32_t* __restrict__ docs, float* __restrict__ loss_rows,
+                                                    float* __restrict__ dz, int nb, int S) {
   __shared__ float red[4];
   const int b = blockIdx.x;
+  const auto live = [&](int s) { return !docs || docs[(int64_t)b * S + s] >= 0; };
   float loss = 0.f;
   for (int c = 0; c < 2; ++c) {
     const float* zc = z + (int64_t)b * S * 2 + c;
     float mx = -INFINITY;
-    for (int s = threadIdx.x; s < S; s += 256) mx = fmaxf(mx, zc[2 * s]);
+    for (int s = threadIdx.x; s < S; s += 256) mx = live(s) ? fmaxf(mx, zc[2 * s]) : mx;
     mx = block_max<4>(mx, red);
     float sum = 0.f;
-    for (int s = threadIdx.x; s < S; s += 256) sum += expf(zc[2 * s] - mx);
+    for (int s = threadIdx.x; s < S; s += 256) sum += live(s) ? expf(zc[2 * s] - mx) : 0.f;
     sum = block_sum<4>(sum, red);
     const float lse = mx + logf(sum);
     const int lab = clamp_id(labels[2 * b + c], S);
-    loss += 0.5f * (lse - zc[2 * lab]);
+    const bool counts = live(lab);
+    loss += counts ? 0.5f * (lse - zc[2 * lab]) : 0.f;
     const float sc = 0.5f / (float)nb;
     for (int s = threadIdx.x; s < S; s += 256)
-      dz[((int64_t)b * S + s) * 2 + c] = (expf(zc[2 * s] - lse) - (s == lab ? 1.f : 0.f)) * sc;
+      dz[((int64_t)b * S + s) * 2 + c] = counts && live(s) ? (expf(zc[2 * s] - lse) - (s == lab ? 1.f : 0.f)) * sc : 0.f;
   }
   if (threadIdx.x == 0) loss_rows[b] = loss;
 }
-void qa_ce(int dt, const float* z, const int32_t* labels, float* loss_rows, float* dz, int nb, int S, hipStream_t st) {
+void qa_ce(int dt, const float* z, const int32_t* labels, const int32_t* docs, float* loss_rows, float* dz, int nb, int S, hipStream_t st) {
   (void)dt;
-  hipLaunchKernelGGL(qa_ce_kernel, dim3(nb), dim3(256), 0, st, z, labels, loss_rows, dz, nb, S);
+  hipLaunchKernelGGL(qa_ce_kernel, dim3(nb), dim3(256), 0, st, z, labels, docs, loss_rows, dz, nb, S);
 }
 
 constexpr int kQaBlocks = 512;   // workgroups (partial rows) at most; four waves each, one row per wave at a time

@@ -105,3 +105,20 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
         with pytest.raises(binding.PtError) as e:
             call()
         assert e.value.status == binding.PT_EINVAL, at
+
+
+def test_checkpoints_shrink_the_work_arena():
+    """act8: per token and block the activation and its derivative (2 F elements) become F codes and one exponent for 32 of them,
+    and one buffer of F elements serves all blocks."""
+    from paper_2102_03161_amd import synth
+    for name in ("vit_b16", "bert_base_qa"):
+        w = synth.workload(name)
+        plain, small = (binding.query_arena_bytes(binding.make_config(w, act8=a)) for a in (False, True))
+        T, F, L = w["B"] * w["S"], w["F"], w["L"]
+        assert plain[:2] == small[:2] and plain[3] == small[3]
+        saved = (L + 1) * 2 * 2 * T * F - (L * T * (F + F // 32) + 2 * T * F)    # the frozen prefix's slot had both as well
+        assert abs((plain[2] - small[2]) - saved) <= 4 * 256 * (L + 1)           # rounded up to 256 bytes
+    cfg = binding.make_config(w)
+    cfg.act8 = 2
+    with pytest.raises(binding.PtError):
+        binding.query_arena_bytes(cfg)
