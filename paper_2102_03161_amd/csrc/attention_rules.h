@@ -75,9 +75,10 @@ __device__ __forceinline__ int rule_wave_min(int v) {
 }
 __device__ __forceinline__ int rule_wave_max(int v) { return ~rule_wave_min(~v); }
 
-// The tiles that a workgroup of four waves visits, each wave owning ROWS rows: entries tile << 8 | whole bits << 4 | needed bits.
-// In LDS: the least and the largest document of each wave's rows and of each tile (the sign of the largest says that padding or
-// several documents are among them), then, in place of the tiles' least, the entries.  A tile is needed by a wave whose range of
+// The tiles that a workgroup of four waves visits, each wave owning ROWS rows: entries tile << 9 | plain << 8 | whole bits << 4 |
+// needed bits.  plain: all its rows exist and none is padding.
+// In LDS: the least and the largest document of each wave's rows and of each tile (the sign of the least says that padding is among
+// them, that of the largest that padding or several documents are), then, in place of the tiles' least, the entries.  A tile is needed by a wave whose range of
 // documents meets its own and whose positions reach it; it is whole if both are one and the same document and all positions of
 // the wave see all of the tile.
 template <int ROWS>
@@ -89,16 +90,18 @@ struct RuleList {
   __device__ __forceinline__ int* lo() const { return base + 12; }              // [tiles + 2]: the loop reads one entry ahead
   __device__ __forceinline__ int* hi() const { return base + 12 + tiles + 2; }
   __device__ __forceinline__ int entry(int it) const { return __builtin_amdgcn_readfirstlane(lo()[it]); }
+  static __device__ __forceinline__ int tile(int e) { return e >> 9; }
   static __device__ __forceinline__ bool needed(int e, int wave) { return e >> wave & 1; }
   static __device__ __forceinline__ bool whole(int e, int wave) { return e >> (4 + wave) & 1; }
+  static __device__ __forceinline__ bool plain(int e) { return e >> 8 & 1; }
 
   // raw: the lane's document (below 0: padding); in: it is of a row that exists
   __device__ __forceinline__ void range(int* lo_, int* hi_, int raw, bool in, int lane) const {
     const bool on = in && raw >= 0;
     const int least = rule_wave_min(on ? raw : 0x7fffffff), most = rule_wave_max(on ? raw : -1);
-    const bool mixed = least != most || __any(in && !on);
+    const bool pad = __any(in && !on), mixed = least != most || pad;
     if (lane == 0) {
-      *lo_ = least;
+      *lo_ = pad ? least | (int)0x80000000 : least;
       *hi_ = mixed ? most | (int)0x80000000 : most;
     }
   }
@@ -129,14 +132,14 @@ struct RuleList {
       int count = 0;
       for (int t0 = 0; t0 < tiles; t0 += 64) {
         const int t = t0 + lane, r0 = t * kRuleTile, r1 = r0 + kRuleTile - 1;
-        const int tlo = docs && t < tiles ? lo()[t] : 0, thi_ = docs && t < tiles ? hi()[t] : 0;
-        const int thi = thi_ & 0x7fffffff;
+        const int tlo_ = docs && t < tiles ? lo()[t] : 0, thi_ = docs && t < tiles ? hi()[t] : 0;
+        const int tlo = tlo_ & 0x7fffffff, thi = thi_ & 0x7fffffff;
         const int lim0 = KEYS ? 0 : rows.lim(g, r0), lim1 = KEYS ? 0 : rows.lim(g, r1 < n ? r1 : n - 1);
         int e = 0;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           const int o0 = (blk * 4 + w) * ROWS, o1 = o0 + ROWS - 1 < m ? o0 + ROWS - 1 : m - 1;
-          const int wlo = docs ? base[2 * w] : 0, whi_ = docs ? base[2 * w + 1] : 0, whi = whi_ & 0x7fffffff;
+          const int wlo = docs ? base[2 * w] & 0x7fffffff : 0, whi_ = docs ? base[2 * w + 1] : 0, whi = whi_ & 0x7fffffff;
           bool need = t < tiles && o0 < m && tlo <= whi && wlo <= thi;
           bool all = thi_ >= 0 && whi_ >= 0 && tlo == wlo;
           if (KEYS) {
@@ -149,7 +152,7 @@ struct RuleList {
           e |= (need ? 1 : 0) << w | (need && all ? 1 : 0) << (4 + w);
         }
         const uint64_t bits = __ballot(e != 0);
-        if (e) lo()[count + __popcll(bits & ((1ull << lane) - 1))] = t << 8 | e;
+        if (e) lo()[count + __popcll(bits & ((1ull << lane) - 1))] = t << 9 | (r1 < n && tlo_ >= 0 ? 1 : 0) << 8 | e;
         count += __popcll(bits);
       }
       if (lane == 0) base[8] = count;

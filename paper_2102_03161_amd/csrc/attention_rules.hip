@@ -20,6 +20,7 @@
 namespace pt {
 
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
 typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 
@@ -50,7 +51,8 @@ __device__ __forceinline__ bf16x8 pack8(const f32x16& a, int first) {
 // DP: the head size rounded up to 64 or 128; columns from dh on are zeros
 template <int DP>
 struct Tile {
-  static constexpr int LD = DP + 8;                   // 16-byte row reads without conflicts
+  // 36 or 72 dwords: neither eight rows of 16-byte reads nor four rows of transposing reads share a bank
+  static constexpr int LD = DP == 64 ? 72 : 144;
   static constexpr int ELEMS = kRuleTile * LD;
   static constexpr int N = kRuleTile * DP / 8 / 256;  // 16-byte pieces per thread
   static constexpr int RSTEP = 256 / (DP / 8);        // rows between a thread's pieces
@@ -96,13 +98,18 @@ struct Tile {
       }
     }
   }
-  // the same for two weights and two results
-  static __device__ __forceinline__ void add2(const bf16* s, int r0, int lane, const f32x16& w, f32x16 (&acc)[DT], const f32x16& w2, f32x16 (&acc2)[DT]) {
+  // the same for two weights and two results; *sum += the first weights as they were rounded, unless null
+  static __device__ __forceinline__ void add2(const bf16* s, int r0, int lane, const f32x16& w, f32x16 (&acc)[DT], const f32x16& w2, f32x16 (&acc2)[DT], float* sum) {
     const int l16 = lane & 15, grp = lane >> 4;
     const bf16* p = s + (r0 + 4 * (grp >> 1) + (l16 >> 2)) * LD + 16 * (grp & 1) + 4 * (l16 & 3);
 #pragma unroll
     for (int ks2 = 0; ks2 < 2; ++ks2) {
       const bf16x8 b = pack8(w, 8 * ks2), b2 = pack8(w2, 8 * ks2);
+      if (sum) {
+        const bf16x2 one = {static_cast<bf16>(1.f), static_cast<bf16>(1.f)};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) *sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{b[2 * e], b[2 * e + 1]}, one, *sum, false);
+      }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         const bf16x8 t = column(p + 16 * ks2 * LD + 32 * dt);
@@ -166,6 +173,10 @@ struct Stream {
         r[x] = *reinterpret_cast<const uint4*>(p + (i < last ? i : last) * ld + (col_ok ? col : 0));
       }
     }
+  }
+  __device__ __forceinline__ void store(bf16* s) const {   // a plain tile and DP columns
+#pragma unroll
+    for (int x = 0; x < T::N; ++x) *reinterpret_cast<uint4*>(s + (row + x * T::RSTEP) * T::LD + col) = r[x];
   }
   __device__ __forceinline__ void store(bf16* s, const bool (&keep)[T::N]) const {
 #pragma unroll
@@ -261,16 +272,22 @@ __global__ __launch_bounds__(256) void rule_fwd_kernel(AttnRuleArgs g) {
   for (int dt = 0; dt < T::DT; ++dt) o[dt] = zero16();
   float m = 0.f, lsum = 0.f;
   auto load = [&](int e) {
-    const int j0 = (e >> 8) * kRuleTile;
+    const int j0 = list.tile(e) * kRuleTile;
     sd.load(j0);
     sk.load(j0, g.Sk);
     sv.load(j0, g.Sk);
   };
   auto store = [&](int e, int at) {
     bool keep[T::N];
-    sd.finish((e >> 8) * kRuleTile, -1, kdoc + at * kRuleTile, sk.col == 0, keep);
-    sk.store(buf + at * 2 * T::ELEMS, keep);
-    sv.store(buf + at * 2 * T::ELEMS + T::ELEMS, keep);
+    sd.finish(list.tile(e) * kRuleTile, -1, kdoc + at * kRuleTile, sk.col == 0, keep);
+    bf16* kb = buf + at * 2 * T::ELEMS;
+    if (list.plain(e) && g.dh == DP) {
+      sk.store(kb);
+      sv.store(kb + T::ELEMS);
+    } else {
+      sk.store(kb, keep);
+      sv.store(kb + T::ELEMS, keep);
+    }
   };
   int e = list.entry(0), next = list.entry(1);
   if (n > 0) { load(e); store(e, 0); }
@@ -279,7 +296,7 @@ __global__ __launch_bounds__(256) void rule_fwd_kernel(AttnRuleArgs g) {
     if (it + 1 < n) load(next);
     if (list.needed(e, wave)) {
       const bf16* kb = buf + (it & 1) * 2 * T::ELEMS;
-      const int j0 = (e >> 8) * kRuleTile;
+      const int j0 = list.tile(e) * kRuleTile;
       const float at = (float)(g.q0 + i - j0 - 4 * half);
       f32x16 s[2];
       // scores less the reference, of the visible pairs; -infinity of the others
@@ -356,7 +373,9 @@ __global__ __launch_bounds__(256) void rule_fwd_kernel(AttnRuleArgs g) {
 // delta_i = dO_i . o_i with o rounded to bf16 is off by 2^-9 of |dO||o|, which for a query with few keys, or one that takes most
 // of the weight, is as large as dS itself.  So the pass uses that value d only to centre dP, and takes out what is left of it:
 // with r_i = sum_j p_ij (dP_ij - d_i), the true delta is d_i + r_i, and dq_i = scale (sum_j w_ij (dP_ij - d_i) k_j - r_i sum_j
-// w_ij k_j), w = p (1 - tanh^2): one more product with the keys' fragments that the pass has in registers anyway.
+// w_ij k_j), w = p (1 - tanh^2): one more product with the keys' fragments that the pass has in registers anyway.  Without a cap
+// r is summed from dS as rounded to bf16 for the product, two to an instruction: the part of those roundings that all keys share,
+// which dS itself, summing to 0, does not have, then cancels.
 // p of 1 means a query that sees one key: dS is exactly 0 then, where dP - delta would leave the rounding of two different sums
 constexpr float kOneKey = 1.f - 1.f / 65536.f;
 
@@ -389,16 +408,22 @@ __global__ __launch_bounds__(256) void rule_dq_kernel(AttnRuleArgs g) {
   for (int dt = 0; dt < T::DT; ++dt) { dq[dt] = zero16(); wk[dt] = zero16(); }
   float rest = 0.f;
   auto load = [&](int e) {
-    const int j0 = (e >> 8) * kRuleTile;
+    const int j0 = list.tile(e) * kRuleTile;
     sd.load(j0);
     sk.load(j0, g.Sk);
     sv.load(j0, g.Sk);
   };
   auto store = [&](int e, int at) {
     bool keep[T::N];
-    sd.finish((e >> 8) * kRuleTile, -1, kdoc + at * kRuleTile, sk.col == 0, keep);
-    sk.store(buf + at * 2 * T::ELEMS, keep);
-    sv.store(buf + at * 2 * T::ELEMS + T::ELEMS, keep);
+    sd.finish(list.tile(e) * kRuleTile, -1, kdoc + at * kRuleTile, sk.col == 0, keep);
+    bf16* kb = buf + at * 2 * T::ELEMS;
+    if (list.plain(e) && g.dh == DP) {
+      sk.store(kb);
+      sv.store(kb + T::ELEMS);
+    } else {
+      sk.store(kb, keep);
+      sv.store(kb + T::ELEMS, keep);
+    }
   };
   int e = list.entry(0), next = list.entry(1);
   if (n > 0) { load(e); store(e, 0); }
@@ -407,7 +432,7 @@ __global__ __launch_bounds__(256) void rule_dq_kernel(AttnRuleArgs g) {
     if (it + 1 < n) load(next);
     if (list.needed(e, wave)) {
       const bf16* kb = buf + (it & 1) * 2 * T::ELEMS;
-      const int j0 = (e >> 8) * kRuleTile;
+      const int j0 = list.tile(e) * kRuleTile;
       const bool whole = list.whole(e, wave);
       const float at = (float)(g.q0 + i - j0 - 4 * half);
       const int far = lim - j0 - 4 * half;
@@ -440,14 +465,14 @@ __global__ __launch_bounds__(256) void rule_dq_kernel(AttnRuleArgs g) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
           dp[v] *= w[v];
-          rest += dp[v];
           if (MOD & 1) {
+            rest += dp[v];
             const float f = 4.f * s[v] * (1.f - s[v]);
             dp[v] *= f;
             w[v] *= f;
           }
         }
-        T::add2(kb, 32 * st, lane, dp, dq, w, wk);
+        T::add2(kb, 32 * st, lane, dp, dq, w, wk, (MOD & 1) ? nullptr : &rest);
       }
     }
     if (it + 1 < n) store(next, (it + 1) & 1);
@@ -497,7 +522,7 @@ __global__ __launch_bounds__(256) void rule_dkv_kernel(AttnRuleArgs g) {
     const float* delta = g.delta + ((int64_t)b * g.H + h) * g.Sq;
     float rl = 0.f, rdl = 0.f;
     auto load = [&](int e) {
-      const int i0 = (e >> 8) * kRuleTile;
+      const int i0 = list.tile(e) * kRuleTile;
       sd.load(i0);
       if (tid < kRuleTile) {
         const int r = i0 + tid < g.Sq ? i0 + tid : g.Sq - 1;
@@ -508,7 +533,7 @@ __global__ __launch_bounds__(256) void rule_dkv_kernel(AttnRuleArgs g) {
       so.load(i0, g.Sq);
     };
     auto store = [&](int e, int at) {
-      const int i0 = (e >> 8) * kRuleTile;
+      const int i0 = list.tile(e) * kRuleTile;
       bool keep[T::N];
       sd.finish(i0, -2, info + at * 2 * kRuleTile, sq.col == 0, keep);
       if (tid < kRuleTile) {
@@ -517,8 +542,14 @@ __global__ __launch_bounds__(256) void rule_dkv_kernel(AttnRuleArgs g) {
         stat[at * 2 * kRuleTile + kRuleTile + tid] = rdl;
         info[at * 2 * kRuleTile + kRuleTile + tid] = rows.lim(g, i0 + tid);
       }
-      sq.store(buf + at * 2 * T::ELEMS, keep);
-      so.store(buf + at * 2 * T::ELEMS + T::ELEMS, keep);
+      bf16* qb = buf + at * 2 * T::ELEMS;
+      if (list.plain(e) && g.dh == DP) {
+        sq.store(qb);
+        so.store(qb + T::ELEMS);
+      } else {
+        sq.store(qb, keep);
+        so.store(qb + T::ELEMS, keep);
+      }
     };
     int e = first, next = list.entry(1);
     if (n > 0) {
@@ -534,7 +565,7 @@ __global__ __launch_bounds__(256) void rule_dkv_kernel(AttnRuleArgs g) {
         const float* st2 = stat + (it & 1) * 2 * kRuleTile;
         const int* inf = info + (it & 1) * 2 * kRuleTile;
         const bool whole = list.whole(e, wave);
-        const float at = (float)(g.q0 + (e >> 8) * kRuleTile - j + 4 * half);
+        const float at = (float)(g.q0 + list.tile(e) * kRuleTile - j + 4 * half);
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
           f32x16 s = T::dot(qb, 32 * st, lane, kf);

@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_fwd_f32_kernel(Attn
   float m = -1e30f, sum = 0.f;
   int rd = 0;
   auto load = [&](int it) {
-    const int j0 = (list.entry(it) >> 8) * kRuleTile;
+    const int j0 = list.tile(list.entry(it)) * kRuleTile;
     A::load(kp, g.k.t, j0, g.Sk, g.dh, tid, rk);
     A::load(vp, g.v.t, j0, g.Sk, g.dh, tid, rv);
     if (tid < kRuleTile) rd = rows.k_raw(g, j0 + tid);
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_fwd_f32_kernel(Attn
     __syncthreads();
     if (it + 1 < n) load(it + 1);
     if (!list.needed(list.entry(it), wave)) continue;
-    const int j0 = (list.entry(it) >> 8) * kRuleTile;
+    const int j0 = list.tile(list.entry(it)) * kRuleTile;
     const float at = (float)(g.q0 + i - j0);
     f32x4 s[4];
     float mx = m;
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
     const float dl = on ? g.delta[((int64_t)b * g.H + h) * g.Sq + i] : 0.f;
     int rd = 0;
     auto load = [&](int it) {
-      const int j0 = (list.entry(it) >> 8) * kRuleTile;
+      const int j0 = list.tile(list.entry(it)) * kRuleTile;
       A::load(kp, g.k.t, j0, g.Sk, g.dh, tid, rx);
       A::load(vp, g.v.t, j0, g.Sk, g.dh, tid, ry);
       if (tid < kRuleTile) rd = rows.k_raw(g, j0 + tid);
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
       __syncthreads();
       if (it + 1 < n) load(it + 1);
       if (!list.needed(list.entry(it), wave)) continue;
-      const int j0 = (list.entry(it) >> 8) * kRuleTile;
+      const int j0 = list.tile(list.entry(it)) * kRuleTile;
       const float at = (float)(g.q0 + i - j0);
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
   int rd = 0, rlim = 0;
   float rl = 0.f, rdl = 0.f;
   auto load = [&](int it) {
-    const int h = hk * G + it / n, i0 = (list.entry(it % n) >> 8) * kRuleTile;
+    const int h = hk * G + it / n, i0 = list.tile(list.entry(it % n)) * kRuleTile;
     A::load(static_cast<const float*>(g.q.p) + b * g.q.b + h * g.q.h, g.q.t, i0, g.Sq, g.dh, tid, rx);
     A::load(static_cast<const float*>(g.d_o.p) + b * g.d_o.b + h * g.d_o.h, g.d_o.t, i0, g.Sq, g.dh, tid, ry);
     if (tid < kRuleTile) {
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
     const int item = it % n;
     if (!list.needed(list.entry(item), wave)) continue;
     const ScoreF sc(g, hk * G + it / n);
-    const float at = (float)(g.q0 + (list.entry(item) >> 8) * kRuleTile - j);
+    const float at = (float)(g.q0 + list.tile(list.entry(item)) * kRuleTile - j);
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       f32x4 p = A::dot(xs, 16 * x, l, gr, a0);
