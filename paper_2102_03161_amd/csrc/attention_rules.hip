@@ -48,16 +48,25 @@ __device__ __forceinline__ bf16x8 pack8(const f32x16& a, int first) {
   return r;
 }
 
-// DP: the head size rounded up to 64 or 128; columns from dh on are zeros
+__device__ __forceinline__ unsigned lds_addr(const void* p) {
+  return (unsigned)(size_t)((__attribute__((address_space(3))) const void*)(p));
+}
+typedef __attribute__((address_space(3))) const bf16x8 lds8;
+typedef __attribute__((address_space(3))) bf16x4 lds4;
+
+// DP: the head size rounded up to 64 or 128; columns from dh on are zeros.
+// A tile in LDS is 64 rows of DP values without padding, as the direct loads from global memory leave it; the 16-byte pieces of a row
+// are permuted, piece c lies at c ^ swizzle(row), so that neither eight rows' 16-byte reads of one piece nor the four rows of a
+// transposing read share a bank.
 template <int DP>
 struct Tile {
-  // 36 or 72 dwords: neither eight rows of 16-byte reads nor four rows of transposing reads share a bank
-  static constexpr int LD = DP == 64 ? 72 : 144;
-  static constexpr int ELEMS = kRuleTile * LD;
+  static constexpr int RB = DP * 2;                   // bytes of a row
+  static constexpr int BYTES = kRuleTile * RB;
   static constexpr int N = kRuleTile * DP / 8 / 256;  // 16-byte pieces per thread
-  static constexpr int RSTEP = 256 / (DP / 8);        // rows between a thread's pieces
+  static constexpr int PR = DP / 8;                   // pieces of a row
   static constexpr int KS = DP / 16;                  // k steps of a product over the head size
   static constexpr int DT = DP / 32;                  // 32-column tiles of the head size
+  static __device__ __forceinline__ int swizzle(int row) { return DP == 64 ? row & 7 : (row & 7) * 2; }
   // the wave's own row as an operand: columns 16 ks + 8 half .. + 7
   static __device__ __forceinline__ void own(const bf16* row, bool ok, int dh, int half, bf16x8 (&f)[KS]) {
 #pragma unroll
@@ -68,40 +77,42 @@ struct Tile {
       f[ks] = t.v;
     }
   }
-  // rows r0 .. r0 + 31 of the tile times the owned rows
-  static __device__ __forceinline__ f32x16 dot(const bf16* s, int r0, int lane, const bf16x8 (&f)[KS]) {
+  // a lane's address in a tile at LDS address s for dot() and for add()
+  static __device__ __forceinline__ unsigned row_addr(unsigned s, int lane) {
+    return s + (lane & 31) * RB + (((lane >> 5) ^ swizzle(lane)) << 4);
+  }
+  static __device__ __forceinline__ unsigned col_addr(unsigned s, int lane) {
+    const int l16 = lane & 15, grp = lane >> 4, row = 4 * (grp >> 1) + (l16 >> 2), piece = 2 * (grp & 1) + ((l16 & 3) >> 1);
+    return s + row * RB + ((piece ^ swizzle(row)) << 4) + 8 * (l16 & 1);
+  }
+  // rows r0 .. r0 + 31 of the tile times the owned rows; at: row_addr()
+  static __device__ __forceinline__ f32x16 dot(unsigned at, int r0, const bf16x8 (&f)[KS]) {
     f32x16 acc = zero16();
-    const bf16* p = s + (r0 + (lane & 31)) * LD + (lane >> 5) * 8;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(p + 16 * ks), f[ks], acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(lds8*)(size_t)((at ^ (32 * ks)) + r0 * RB), f[ks], acc, 0, 0, 0);
     return acc;
   }
-  static __device__ __forceinline__ bf16x8 column(const bf16* q) {
-    typedef __attribute__((address_space(3))) bf16x4 lds4;
+  // the transposing LDS read hands a lane four consecutive rows of one column, in the order in which the weights of add() stand in
+  // the accumulator
+  static __device__ __forceinline__ bf16x8 column(unsigned at, int r0, int dt) {
+    const unsigned p = at ^ (64 * dt);
     union { bf16x4 h[2]; bf16x8 v; } t;
-    t.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(q));
-    t.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(q + 8 * LD));
+    t.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(size_t)(p + r0 * RB));
+    t.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(size_t)(p + (r0 + 8) * RB));
     return t.v;
   }
-  // acc[dt] (columns 32 dt + .. of the owned rows) += sum over rows r0 .. r0 + 31 of tile row x weight; the transposing LDS read
-  // hands a lane four consecutive rows of one column, in the order in which the weights stand in the accumulator
-  static __device__ __forceinline__ void add(const bf16* s, int r0, int lane, const f32x16& w, f32x16 (&acc)[DT]) {
-    const int l16 = lane & 15, grp = lane >> 4;
-    const bf16* p = s + (r0 + 4 * (grp >> 1) + (l16 >> 2)) * LD + 16 * (grp & 1) + 4 * (l16 & 3);
+  // acc[dt] (columns 32 dt + .. of the owned rows) += sum over rows r0 .. r0 + 31 of tile row x weight; at: col_addr()
+  static __device__ __forceinline__ void add(unsigned at, int r0, const f32x16& w, f32x16 (&acc)[DT]) {
 #pragma unroll
     for (int ks2 = 0; ks2 < 2; ++ks2) {
       const bf16x8 b = pack8(w, 8 * ks2);
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(column(p + 16 * ks2 * LD + 32 * dt), b, acc[dt], 0, 0, 0);
-      }
+      for (int dt = 0; dt < DT; ++dt) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(column(at, r0 + 16 * ks2, dt), b, acc[dt], 0, 0, 0);
     }
   }
   // the same for two weights and two results; *sum += the first weights as they were rounded, unless null
-  static __device__ __forceinline__ void add2(const bf16* s, int r0, int lane, const f32x16& w, f32x16 (&acc)[DT], const f32x16& w2, f32x16 (&acc2)[DT], float* sum) {
-    const int l16 = lane & 15, grp = lane >> 4;
-    const bf16* p = s + (r0 + 4 * (grp >> 1) + (l16 >> 2)) * LD + 16 * (grp & 1) + 4 * (l16 & 3);
+  static __device__ __forceinline__ void add2(unsigned at, int r0, const f32x16& w, f32x16 (&acc)[DT], const f32x16& w2, f32x16 (&acc2)[DT], float* sum) {
 #pragma unroll
     for (int ks2 = 0; ks2 < 2; ++ks2) {
       const bf16x8 b = pack8(w, 8 * ks2), b2 = pack8(w2, 8 * ks2);
@@ -112,7 +123,7 @@ struct Tile {
       }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        const bf16x8 t = column(p + 16 * ks2 * LD + 32 * dt);
+        const bf16x8 t = column(at, r0 + 16 * ks2, dt);
         acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t, b, acc[dt], 0, 0, 0);
         acc2[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t, b2, acc2[dt], 0, 0, 0);
       }
@@ -143,47 +154,66 @@ struct Tile {
   }
 };
 
-// One streamed matrix: this thread's pieces of a tile, loaded while the tile before is multiplied.  Rows behind the last are read
-// as the last one and columns behind the head size as column 0, so that no load hangs on a branch; store() zeroes both, and padding.
+// 16 bytes a lane from global memory to LDS, lanes next to each other from `to` on, without a register in between.  Written as
+// assembly because the compiler, for the builtin, waits for such loads in front of every LDS read; all of them are waited for by
+// loads_done(), in front of the barrier behind which the tile is read.
+__device__ __forceinline__ void load_to_lds(unsigned to, const void* from) {
+  unsigned kept;   // m0 as it was: the compiler may hold something in it
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
+               : "=&s"(kept) : "s"(to), "v"(from) : "memory");
+}
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Two streamed matrices (K and V, or Q and dO): a thread's N pieces of a tile of each, tiles in LDS next to each other.  Rows behind
+// the last are read as the last one; clear() zeroes them, and padding, once they have arrived.  Columns behind the head size are
+// never loaded: the buffers start as zeros where there are any.
 template <int DP>
-struct Stream {
+struct Streams {
   typedef Tile<DP> T;
-  const bf16* base;
-  int64_t ld, at;       // at: of the thread's first piece in a whole tile
-  int row, col;
-  bool col_ok;
-  uint4 r[T::N];
-  __device__ __forceinline__ Stream(const HeadView& v, int b, int h, int tid, int dh) {
-    base = static_cast<const bf16*>(v.p) + b * v.b + h * v.h;
-    ld = v.t;
-    row = tid / (DP / 8);
-    col = (tid % (DP / 8)) * 8;
-    col_ok = col < dh;
-    at = row * ld + (col_ok ? col : 0);
+  static constexpr int RI = 64 / T::PR;   // rows of one load of a wave
+  const bf16* base[2];
+  int64_t ld[2];
+  int row, piece;    // of the first load
+  __device__ __forceinline__ Streams(const HeadView& x, int hx, const HeadView& y, int hy, int b, int wave, int lane) {
+    base[0] = static_cast<const bf16*>(x.p) + b * x.b + hx * x.h;
+    base[1] = static_cast<const bf16*>(y.p) + b * y.b + hy * y.h;
+    ld[0] = x.t;
+    ld[1] = y.t;
+    row = wave * T::N * RI + lane / T::PR;
+    piece = lane % T::PR;
   }
-  __device__ __forceinline__ void load(int r0, int n) {
-    const bf16* p = base + r0 * ld;
-    if (r0 + kRuleTile <= n) {
+  __device__ __forceinline__ int col(int i) const { return 8 * (piece ^ T::swizzle(row + i * RI)); }
+  // to: LDS address of the first tile plus the wave's share, wave * N KB
+  __device__ __forceinline__ void load(unsigned to, int r0, int n, int dh) const {
+    const bool all = r0 + kRuleTile <= n;
 #pragma unroll
-      for (int x = 0; x < T::N; ++x) r[x] = *reinterpret_cast<const uint4*>(p + x * T::RSTEP * ld + at);
-    } else {
+    for (int m = 0; m < 2; ++m) {
+      const bf16* p = base[m] + r0 * ld[m];
 #pragma unroll
-      for (int x = 0; x < T::N; ++x) {
-        const int i = row + x * T::RSTEP, last = n - 1 - r0;
-        r[x] = *reinterpret_cast<const uint4*>(p + (i < last ? i : last) * ld + (col_ok ? col : 0));
+      for (int i = 0; i < T::N; ++i) {
+        int r = row + i * RI;
+        if (!all) r = r < n - 1 - r0 ? r : n - 1 - r0;
+        const bf16* from = p + r * ld[m] + col(i);
+        if (dh == DP || col(i) < dh) load_to_lds(to + m * T::BYTES + i * 1024, from);
       }
     }
   }
-  __device__ __forceinline__ void store(bf16* s) const {   // a plain tile and DP columns
+  __device__ __forceinline__ void clear(unsigned to, int lane, const bool (&keep)[T::N]) const {
+    typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+    typedef __attribute__((address_space(3))) u32x4 lds16;
 #pragma unroll
-    for (int x = 0; x < T::N; ++x) *reinterpret_cast<uint4*>(s + (row + x * T::RSTEP) * T::LD + col) = r[x];
-  }
-  __device__ __forceinline__ void store(bf16* s, const bool (&keep)[T::N]) const {
+    for (int i = 0; i < T::N; ++i)
+      if (!keep[i])
 #pragma unroll
-    for (int x = 0; x < T::N; ++x)
-      *reinterpret_cast<uint4*>(s + (row + x * T::RSTEP) * T::LD + col) = keep[x] && col_ok ? r[x] : make_uint4(0, 0, 0, 0);
+        for (int m = 0; m < 2; ++m) *(lds16*)(size_t)(to + m * T::BYTES + i * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
   }
 };
+template <int DP>
+__device__ __forceinline__ void zero_tiles(unsigned char* smem, int dh) {   // both buffers' two tiles; a barrier follows
+  if (dh == DP) return;
+  for (int i = threadIdx.x; i < 4 * Tile<DP>::BYTES / 16; i += 256) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+  __syncthreads();
+}
 // the documents of the same pieces' rows
 template <int DP>
 struct StreamDocs {
@@ -191,21 +221,21 @@ struct StreamDocs {
   const int32_t* d;
   int n, row;
   int raw[T::N];
-  __device__ __forceinline__ StreamDocs(const int32_t* docs, int n_, int tid) : d(docs), n(n_), row(tid / (DP / 8)) {}
+  __device__ __forceinline__ StreamDocs(const int32_t* docs, int n_, int row_) : d(docs), n(n_), row(row_) {}
   __device__ __forceinline__ void load(int r0) {
     if (d) {
 #pragma unroll
       for (int x = 0; x < T::N; ++x) {
-        const int i = r0 + row + x * T::RSTEP;
+        const int i = r0 + row + x * Streams<DP>::RI;
         raw[x] = d[i < n ? i : n - 1];
       }
     }
   }
-  // keep: the row exists and is no padding; its document (as the owned side compares it) goes to docs unless null
+  // keep: the row exists and is no padding; first: this thread writes the row's document (as the owned side compares it)
   __device__ __forceinline__ void finish(int r0, int none, int* docs, bool first, bool (&keep)[T::N]) const {
 #pragma unroll
     for (int x = 0; x < T::N; ++x) {
-      const int i = row + x * T::RSTEP, v = d ? raw[x] : 0;
+      const int i = row + x * Streams<DP>::RI, v = d ? raw[x] : 0;
       keep[x] = r0 + i < n && v >= 0;
       if (first) docs[i] = keep[x] ? v : none;
     }
@@ -249,8 +279,7 @@ template <int DP, int MOD>
 __global__ __launch_bounds__(256) void rule_fwd_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  bf16* buf = reinterpret_cast<bf16*>(smem);                                  // [2][K tile, V tile]
-  int* kdoc = reinterpret_cast<int*>(buf + 4 * T::ELEMS);                     // [2][64]
+  int* kdoc = reinterpret_cast<int*>(smem + 4 * T::BYTES);                    // [2][64], behind [2][K tile, V tile]
   const RuleList<32> list(kdoc + 2 * kRuleTile, g.Sk);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
   const int nqb = (g.Sq + 127) / 128;
@@ -264,38 +293,33 @@ __global__ __launch_bounds__(256) void rule_fwd_kernel(AttnRuleArgs g) {
   bf16x8 qf[T::KS];
   T::own(static_cast<const bf16*>(g.q.p) + b * g.q.b + (int64_t)i * g.q.t + h * g.q.h, on, g.dh, half, qf);
   const int n = list.build<true>(g, rows, wave, lane, u.blk, qd, ok);
-  Stream<DP> sk(g.k, b, hk, tid, g.dh), sv(g.v, b, hk, tid, g.dh);
-  StreamDocs<DP> sd(rows.k, g.Sk, tid);
+  const Streams<DP> kv(g.k, hk, g.v, hk, b, wave, lane);
+  StreamDocs<DP> sd(rows.k, g.Sk, kv.row);
+  const unsigned lds = lds_addr(smem), mine = lds + wave * T::N * 1024;
   const Score sc(g, h);
   f32x16 o[T::DT];
 #pragma unroll
   for (int dt = 0; dt < T::DT; ++dt) o[dt] = zero16();
   float m = 0.f, lsum = 0.f;
-  auto load = [&](int e) {
+  auto load = [&](int e, int at) {
     const int j0 = list.tile(e) * kRuleTile;
     sd.load(j0);
-    sk.load(j0, g.Sk);
-    sv.load(j0, g.Sk);
+    kv.load(mine + at * 2 * T::BYTES, j0, g.Sk, g.dh);
   };
-  auto store = [&](int e, int at) {
+  auto finish = [&](int e, int at) {
     bool keep[T::N];
-    sd.finish(list.tile(e) * kRuleTile, -1, kdoc + at * kRuleTile, sk.col == 0, keep);
-    bf16* kb = buf + at * 2 * T::ELEMS;
-    if (list.plain(e) && g.dh == DP) {
-      sk.store(kb);
-      sv.store(kb + T::ELEMS);
-    } else {
-      sk.store(kb, keep);
-      sv.store(kb + T::ELEMS, keep);
-    }
+    sd.finish(list.tile(e) * kRuleTile, -1, kdoc + at * kRuleTile, kv.piece == 0, keep);
+    loads_done();
+    if (!list.plain(e)) kv.clear(mine + at * 2 * T::BYTES, lane, keep);
   };
   int e = list.entry(0), next = list.entry(1);
-  if (n > 0) { load(e); store(e, 0); }
+  zero_tiles<DP>(smem, g.dh);
+  if (n > 0) { load(e, 0); finish(e, 0); }
   for (int it = 0; it < n; ++it) {
     __syncthreads();
-    if (it + 1 < n) load(next);
+    if (it + 1 < n) load(next, (it + 1) & 1);
     if (list.needed(e, wave)) {
-      const bf16* kb = buf + (it & 1) * 2 * T::ELEMS;
+      const unsigned kb = lds + (it & 1) * 2 * T::BYTES;
       const int j0 = list.tile(e) * kRuleTile;
       const float at = (float)(g.q0 + i - j0 - 4 * half);
       f32x16 s[2];
@@ -303,7 +327,7 @@ __global__ __launch_bounds__(256) void rule_fwd_kernel(AttnRuleArgs g) {
       auto scores = [&]() {
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
-          s[st] = T::dot(kb, 32 * st, lane, qf);
+          s[st] = T::dot(T::row_addr(kb, lane), 32 * st, qf);
 #pragma unroll
           for (int v = 0; v < 16; ++v) s[st][v] = sc.at<MOD>((MOD & 1) ? sc.bend(s[st][v]) : s[st][v], at - (float)(32 * st + acc_row(v)), -m);
         }
@@ -356,9 +380,9 @@ __global__ __launch_bounds__(256) void rule_fwd_kernel(AttnRuleArgs g) {
       }
       lsum += sum + half_swap(sum);
 #pragma unroll
-      for (int st = 0; st < 2; ++st) T::add(kb + T::ELEMS, 32 * st, lane, s[st], o);
+      for (int st = 0; st < 2; ++st) T::add(T::col_addr(kb + T::BYTES, lane), 32 * st, s[st], o);
     }
-    if (it + 1 < n) store(next, (it + 1) & 1);
+    if (it + 1 < n) finish(next, (it + 1) & 1);
     e = next;
     next = list.entry(it + 2 <= list.tiles ? it + 2 : list.tiles);
   }
@@ -383,8 +407,7 @@ template <int DP, int MOD>
 __global__ __launch_bounds__(256) void rule_dq_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  bf16* buf = reinterpret_cast<bf16*>(smem);
-  int* kdoc = reinterpret_cast<int*>(buf + 4 * T::ELEMS);
+  int* kdoc = reinterpret_cast<int*>(smem + 4 * T::BYTES);
   const RuleList<32> list(kdoc + 2 * kRuleTile, g.Sk);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
   const int nqb = (g.Sq + 127) / 128;
@@ -400,46 +423,41 @@ __global__ __launch_bounds__(256) void rule_dq_kernel(AttnRuleArgs g) {
   const float nlse = on ? -rule_lse2(g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i]) : -INFINITY;
   const float dl = T::own_dot(static_cast<const bf16*>(g.o.p) + b * g.o.b + (int64_t)i * g.o.t + h * g.o.h, on, g.dh, half, dof);
   const int n = list.build<true>(g, rows, wave, lane, u.blk, qd, ok);
-  Stream<DP> sk(g.k, b, hk, tid, g.dh), sv(g.v, b, hk, tid, g.dh);
-  StreamDocs<DP> sd(rows.k, g.Sk, tid);
+  const Streams<DP> kv(g.k, hk, g.v, hk, b, wave, lane);
+  StreamDocs<DP> sd(rows.k, g.Sk, kv.row);
+  const unsigned lds = lds_addr(smem), mine = lds + wave * T::N * 1024;
   const Score sc(g, h);
   f32x16 dq[T::DT], wk[T::DT];
 #pragma unroll
   for (int dt = 0; dt < T::DT; ++dt) { dq[dt] = zero16(); wk[dt] = zero16(); }
   float rest = 0.f;
-  auto load = [&](int e) {
+  auto load = [&](int e, int at) {
     const int j0 = list.tile(e) * kRuleTile;
     sd.load(j0);
-    sk.load(j0, g.Sk);
-    sv.load(j0, g.Sk);
+    kv.load(mine + at * 2 * T::BYTES, j0, g.Sk, g.dh);
   };
-  auto store = [&](int e, int at) {
+  auto finish = [&](int e, int at) {
     bool keep[T::N];
-    sd.finish(list.tile(e) * kRuleTile, -1, kdoc + at * kRuleTile, sk.col == 0, keep);
-    bf16* kb = buf + at * 2 * T::ELEMS;
-    if (list.plain(e) && g.dh == DP) {
-      sk.store(kb);
-      sv.store(kb + T::ELEMS);
-    } else {
-      sk.store(kb, keep);
-      sv.store(kb + T::ELEMS, keep);
-    }
+    sd.finish(list.tile(e) * kRuleTile, -1, kdoc + at * kRuleTile, kv.piece == 0, keep);
+    loads_done();
+    if (!list.plain(e)) kv.clear(mine + at * 2 * T::BYTES, lane, keep);
   };
   int e = list.entry(0), next = list.entry(1);
-  if (n > 0) { load(e); store(e, 0); }
+  zero_tiles<DP>(smem, g.dh);
+  if (n > 0) { load(e, 0); finish(e, 0); }
   for (int it = 0; it < n; ++it) {
     __syncthreads();
-    if (it + 1 < n) load(next);
+    if (it + 1 < n) load(next, (it + 1) & 1);
     if (list.needed(e, wave)) {
-      const bf16* kb = buf + (it & 1) * 2 * T::ELEMS;
+      const unsigned kb = lds + (it & 1) * 2 * T::BYTES;
       const int j0 = list.tile(e) * kRuleTile;
       const bool whole = list.whole(e, wave);
       const float at = (float)(g.q0 + i - j0 - 4 * half);
       const int far = lim - j0 - 4 * half;
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
-        f32x16 s = T::dot(kb, 32 * st, lane, qf);
-        f32x16 dp = T::dot(kb + T::ELEMS, 32 * st, lane, dof);
+        f32x16 s = T::dot(T::row_addr(kb, lane), 32 * st, qf);
+        f32x16 dp = T::dot(T::row_addr(kb + T::BYTES, lane), 32 * st, dof);
         f32x16 w;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
@@ -472,10 +490,10 @@ __global__ __launch_bounds__(256) void rule_dq_kernel(AttnRuleArgs g) {
             w[v] *= f;
           }
         }
-        T::add2(kb, 32 * st, lane, dp, dq, w, wk, (MOD & 1) ? nullptr : &rest);
+        T::add2(T::col_addr(kb, lane), 32 * st, dp, dq, w, wk, (MOD & 1) ? nullptr : &rest);
       }
     }
-    if (it + 1 < n) store(next, (it + 1) & 1);
+    if (it + 1 < n) finish(next, (it + 1) & 1);
     e = next;
     next = list.entry(it + 2 <= list.tiles ? it + 2 : list.tiles);
   }
@@ -493,8 +511,7 @@ template <int DP, int MOD>
 __global__ __launch_bounds__(256) void rule_dkv_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  bf16* buf = reinterpret_cast<bf16*>(smem);                                  // [2][Q tile, dO tile]
-  float* stat = reinterpret_cast<float*>(buf + 4 * T::ELEMS);                 // [2][-lse, delta][64]
+  float* stat = reinterpret_cast<float*>(smem + 4 * T::BYTES);                // [2][-lse, delta][64], behind [2][Q tile, dO tile]
   int* info = reinterpret_cast<int*>(stat + 4 * kRuleTile);                   // [2][document, lim][64]
   const RuleList<32> list(info + 4 * kRuleTile, g.Sq);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
@@ -513,15 +530,17 @@ __global__ __launch_bounds__(256) void rule_dkv_kernel(AttnRuleArgs g) {
 #pragma unroll
   for (int dt = 0; dt < T::DT; ++dt) { dk[dt] = zero16(); dv[dt] = zero16(); }
   const int first = list.entry(0);
+  const unsigned lds = lds_addr(smem), mine = lds + wave * T::N * 1024;
+  zero_tiles<DP>(smem, g.dh);
   // the heads that share these keys, one after the other
   for (int h = hk * G; h < hk * G + G; ++h) {
-    Stream<DP> sq(g.q, b, h, tid, g.dh), so(g.d_o, b, h, tid, g.dh);
-    StreamDocs<DP> sd(rows.q, g.Sq, tid);
+    const Streams<DP> qo(g.q, h, g.d_o, h, b, wave, lane);
+    StreamDocs<DP> sd(rows.q, g.Sq, qo.row);
     const Score sc(g, h);
     const float* lse = g.lse + (int64_t)b * g.lse_b + (int64_t)h * g.lse_h;
     const float* delta = g.delta + ((int64_t)b * g.H + h) * g.Sq;
     float rl = 0.f, rdl = 0.f;
-    auto load = [&](int e) {
+    auto load = [&](int e, int at) {
       const int i0 = list.tile(e) * kRuleTile;
       sd.load(i0);
       if (tid < kRuleTile) {
@@ -529,47 +548,40 @@ __global__ __launch_bounds__(256) void rule_dkv_kernel(AttnRuleArgs g) {
         rl = lse[r];
         rdl = delta[r];
       }
-      sq.load(i0, g.Sq);
-      so.load(i0, g.Sq);
+      qo.load(mine + at * 2 * T::BYTES, i0, g.Sq, g.dh);
     };
-    auto store = [&](int e, int at) {
+    auto finish = [&](int e, int at) {
       const int i0 = list.tile(e) * kRuleTile;
       bool keep[T::N];
-      sd.finish(i0, -2, info + at * 2 * kRuleTile, sq.col == 0, keep);
+      sd.finish(i0, -2, info + at * 2 * kRuleTile, qo.piece == 0, keep);
       if (tid < kRuleTile) {
         // a row behind the last has probability 0; so has one that sees nothing (padding among them)
         stat[at * 2 * kRuleTile + tid] = i0 + tid < g.Sq ? -rule_lse2(rl) : -INFINITY;
         stat[at * 2 * kRuleTile + kRuleTile + tid] = rdl;
         info[at * 2 * kRuleTile + kRuleTile + tid] = rows.lim(g, i0 + tid);
       }
-      bf16* qb = buf + at * 2 * T::ELEMS;
-      if (list.plain(e) && g.dh == DP) {
-        sq.store(qb);
-        so.store(qb + T::ELEMS);
-      } else {
-        sq.store(qb, keep);
-        so.store(qb + T::ELEMS, keep);
-      }
+      loads_done();
+      if (!list.plain(e)) qo.clear(mine + at * 2 * T::BYTES, lane, keep);
     };
     int e = first, next = list.entry(1);
     if (n > 0) {
       if (h > hk * G) __syncthreads();   // the last tile of the head before may still be read
-      load(e);
-      store(e, 0);
+      load(e, 0);
+      finish(e, 0);
     }
     for (int it = 0; it < n; ++it) {
       __syncthreads();
-      if (it + 1 < n) load(next);
+      if (it + 1 < n) load(next, (it + 1) & 1);
       if (list.needed(e, wave)) {
-        const bf16* qb = buf + (it & 1) * 2 * T::ELEMS;
+        const unsigned qb = lds + (it & 1) * 2 * T::BYTES;
         const float* st2 = stat + (it & 1) * 2 * kRuleTile;
         const int* inf = info + (it & 1) * 2 * kRuleTile;
         const bool whole = list.whole(e, wave);
         const float at = (float)(g.q0 + list.tile(e) * kRuleTile - j + 4 * half);
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
-          f32x16 s = T::dot(qb, 32 * st, lane, kf);
-          f32x16 ds = T::dot(qb + T::ELEMS, 32 * st, lane, vf);
+          f32x16 s = T::dot(T::row_addr(qb, lane), 32 * st, kf);
+          f32x16 ds = T::dot(T::row_addr(qb + T::BYTES, lane), 32 * st, vf);
 #pragma unroll
           for (int g4 = 0; g4 < 4; ++g4) {
             const int r0 = 32 * st + 8 * g4 + 4 * half;
@@ -597,11 +609,11 @@ __global__ __launch_bounds__(256) void rule_dkv_kernel(AttnRuleArgs g) {
               }
             }
           }
-          T::add(qb + T::ELEMS, 32 * st, lane, s, dv);
-          T::add(qb, 32 * st, lane, ds, dk);
+          T::add(T::col_addr(qb + T::BYTES, lane), 32 * st, s, dv);
+          T::add(T::col_addr(qb, lane), 32 * st, ds, dk);
         }
       }
-      if (it + 1 < n) store(next, (it + 1) & 1);
+      if (it + 1 < n) finish(next, (it + 1) & 1);
       e = next;
       next = list.entry(it + 2 <= list.tiles ? it + 2 : list.tiles);
     }
@@ -614,7 +626,7 @@ __global__ __launch_bounds__(256) void rule_dkv_kernel(AttnRuleArgs g) {
 
 template <int DP>
 size_t lds_bytes(int streamed, bool dkv) {
-  return (size_t)4 * Tile<DP>::ELEMS * 2 + (dkv ? 8 : 2) * kRuleTile * 4 + RuleList<32>::ints((streamed + kRuleTile - 1) / kRuleTile) * 4;
+  return (size_t)4 * Tile<DP>::BYTES + (dkv ? 8 : 2) * kRuleTile * 4 + RuleList<32>::ints((streamed + kRuleTile - 1) / kRuleTile) * 4;
 }
 template <typename K>
 hipError_t launch(K kernel, int blocks, size_t lds, const AttnRuleArgs& g, hipStream_t st) {
