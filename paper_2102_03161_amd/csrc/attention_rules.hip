@@ -276,7 +276,7 @@ __device__ __forceinline__ void four(const int* p, int (&x)[4]) {
 constexpr float kGrown = 1099511627776.f;   // 2^40
 
 template <int DP, int MOD>
-__global__ __launch_bounds__(256) void rule_fwd_kernel(AttnRuleArgs g) {
+__global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   int* kdoc = reinterpret_cast<int*>(smem + 4 * T::BYTES);                    // [2][64], behind [2][K tile, V tile]
@@ -340,7 +340,11 @@ __global__ __launch_bounds__(256) void rule_fwd_kernel(AttnRuleArgs g) {
               int kd[4];
               four(kdoc + (it & 1) * kRuleTile + 32 * st + 8 * g4 + 4 * half, kd);
 #pragma unroll
-              for (int x = 0; x < 4; ++x) s[st][4 * g4 + x] = kd[x] == qd && 32 * st + 8 * g4 + x <= far ? s[st][4 * g4 + x] : -INFINITY;
+              for (int x = 0; x < 4; ++x) s[st][4 * g4 + x] = kd[x] == qd ? s[st][4 * g4 + x] : -INFINITY;
+              if (g.order != 0) {   // (rows behind the last have no document)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) s[st][4 * g4 + x] = 32 * st + 8 * g4 + x <= far ? s[st][4 * g4 + x] : -INFINITY;
+              }
             }
         }
       };
@@ -401,10 +405,11 @@ __global__ __launch_bounds__(256) void rule_fwd_kernel(AttnRuleArgs g) {
 // r is summed from dS as rounded to bf16 for the product, two to an instruction: the part of those roundings that all keys share,
 // which dS itself, summing to 0, does not have, then cancels.
 // p of 1 means a query that sees one key: dS is exactly 0 then, where dP - delta would leave the rounding of two different sums
+// (for dq the correction below comes to exactly 0 by itself, but with a cap)
 constexpr float kOneKey = 1.f - 1.f / 65536.f;
 
 template <int DP, int MOD>
-__global__ __launch_bounds__(256) void rule_dq_kernel(AttnRuleArgs g) {
+__global__ __launch_bounds__(256, DP == 64 ? 3 : 1) void rule_dq_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   int* kdoc = reinterpret_cast<int*>(smem + 4 * T::BYTES);
@@ -454,7 +459,7 @@ __global__ __launch_bounds__(256) void rule_dq_kernel(AttnRuleArgs g) {
       const bool whole = list.whole(e, wave);
       const float at = (float)(g.q0 + i - j0 - 4 * half);
       const int far = lim - j0 - 4 * half;
-#pragma unroll
+#pragma unroll 1
       for (int st = 0; st < 2; ++st) {
         f32x16 s = T::dot(T::row_addr(kb, lane), 32 * st, qf);
         f32x16 dp = T::dot(T::row_addr(kb + T::BYTES, lane), 32 * st, dof);
@@ -474,9 +479,10 @@ __global__ __launch_bounds__(256) void rule_dq_kernel(AttnRuleArgs g) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               const int v = 4 * g4 + x;
-              const bool see = kd[x] == qd && 32 * st + 8 * g4 + x <= far;
-              dp[v] = see && !(w[v] >= kOneKey) ? dp[v] : 0.f;
-              w[v] = see ? w[v] : 0.f;
+              // with a cap the correction below is no exact 0 for a query that sees one key
+              if ((MOD & 1) && w[v] >= kOneKey) dp[v] = 0.f;
+              w[v] = kd[x] == qd ? w[v] : 0.f;
+              if (g.order != 0) w[v] = 32 * st + 8 * g4 + x <= far ? w[v] : 0.f;
             }
           }
         }
@@ -508,7 +514,7 @@ __global__ __launch_bounds__(256) void rule_dq_kernel(AttnRuleArgs g) {
 }
 
 template <int DP, int MOD>
-__global__ __launch_bounds__(256) void rule_dkv_kernel(AttnRuleArgs g) {
+__global__ __launch_bounds__(256, DP == 64 ? 3 : 1) void rule_dkv_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   float* stat = reinterpret_cast<float*>(smem + 4 * T::BYTES);                // [2][-lse, delta][64], behind [2][Q tile, dO tile]
@@ -578,7 +584,7 @@ __global__ __launch_bounds__(256) void rule_dkv_kernel(AttnRuleArgs g) {
         const int* inf = info + (it & 1) * 2 * kRuleTile;
         const bool whole = list.whole(e, wave);
         const float at = (float)(g.q0 + list.tile(e) * kRuleTile - j + 4 * half);
-#pragma unroll
+#pragma unroll 1
         for (int st = 0; st < 2; ++st) {
           f32x16 s = T::dot(T::row_addr(qb, lane), 32 * st, kf);
           f32x16 ds = T::dot(T::row_addr(qb + T::BYTES, lane), 32 * st, vf);
@@ -593,21 +599,25 @@ __global__ __launch_bounds__(256) void rule_dkv_kernel(AttnRuleArgs g) {
               const int v = 4 * g4 + x;
               const float r = (MOD & 1) ? sc.bend(s[v]) : s[v];
               s[v] = fast_exp2(sc.at<MOD>(r, at + (float)(32 * st + acc_row(v)), nl[x]));
-              ds[v] = s[v] * (ds[v] - dl[x]);
+              ds[v] -= dl[x];
               if (MOD & 1) ds[v] *= 4.f * r * (1.f - r);
             }
             if (!whole) {
-              int qd[4], lm[4];
+              int qd[4];
               four(inf + r0, qd);
-              four(inf + kRuleTile + r0, lm);
 #pragma unroll
-              for (int x = 0; x < 4; ++x) {
-                const int v = 4 * g4 + x;
-                const bool see = qd[x] == kd && j <= lm[x];
-                ds[v] = see && !(s[v] >= kOneKey) ? ds[v] : 0.f;
-                s[v] = see ? s[v] : 0.f;
+              for (int x = 0; x < 4; ++x) s[4 * g4 + x] = qd[x] == kd ? s[4 * g4 + x] : 0.f;
+              if (g.order != 0) {
+                int lm[4];
+                four(inf + kRuleTile + r0, lm);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) s[4 * g4 + x] = j <= lm[x] ? s[4 * g4 + x] : 0.f;
               }
+#pragma unroll
+              for (int x = 0; x < 4; ++x) ds[4 * g4 + x] = s[4 * g4 + x] >= kOneKey ? 0.f : ds[4 * g4 + x];
             }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) ds[4 * g4 + x] *= s[4 * g4 + x];
           }
           T::add(T::col_addr(qb + T::BYTES, lane), 32 * st, s, dv);
           T::add(T::col_addr(qb, lane), 32 * st, ds, dk);

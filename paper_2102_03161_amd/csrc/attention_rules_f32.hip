@@ -28,15 +28,25 @@ struct ScoreF {
   }
 };
 
-// a staged tile; padding rows (which may hold anything) become zeros
+// Two staged tiles, and the barrier behind which they are read.  Rows that are padding (which may hold anything) or behind the last
+// become zeros: those of a tile that has any wait for the documents, which one wave has just written.
 template <typename A>
-__device__ __forceinline__ void rule_store(float* s, int tid, const f32x4 (&reg)[A::N4], const int* docs) {
+__device__ __forceinline__ void rule_stage(bool plain, float* xs, const f32x4 (&x)[A::N4], float* ys, const f32x4 (&y)[A::N4], int tid, const int* docs) {
+  if (plain) {
+    A::store(xs, tid, x);
+    A::store(ys, tid, y);
+  } else {
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < A::N4; ++i) {
-    int row, d;
-    A::place(tid, i, &row, &d);
-    *reinterpret_cast<f32x4*>(s + row * A::LD + d) = docs[row] >= 0 ? reg[i] : f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < A::N4; ++i) {
+      int row, d;
+      A::place(tid, i, &row, &d);
+      const bool keep = docs[row] >= 0;
+      *reinterpret_cast<f32x4*>(xs + row * A::LD + d) = keep ? x[i] : f32x4{0.f, 0.f, 0.f, 0.f};
+      *reinterpret_cast<f32x4*>(ys + row * A::LD + d) = keep ? y[i] : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
   }
+  __syncthreads();
 }
 
 template <int DP>
@@ -74,10 +84,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_fwd_f32_kernel(Attn
   for (int it = 0; it < n; ++it) {
     __syncthreads();
     if (tid < kRuleTile) kdoc[tid] = RuleRows::k_id(rd);
-    __syncthreads();
-    rule_store<A>(xs, tid, rk, kdoc);
-    rule_store<A>(ys, tid, rv, kdoc);
-    __syncthreads();
+    rule_stage<A>(list.plain(list.entry(it)), xs, rk, ys, rv, tid, kdoc);
     if (it + 1 < n) load(it + 1);
     if (!list.needed(list.entry(it), wave)) continue;
     const int j0 = list.tile(list.entry(it)) * kRuleTile;
@@ -162,10 +169,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
     for (int it = 0; it < n; ++it) {
       __syncthreads();
       if (tid < kRuleTile) docs[tid] = RuleRows::k_id(rd);
-      __syncthreads();
-      rule_store<A>(xs, tid, rx, docs);
-      rule_store<A>(ys, tid, ry, docs);
-      __syncthreads();
+      rule_stage<A>(list.plain(list.entry(it)), xs, rx, ys, ry, tid, docs);
       if (it + 1 < n) load(it + 1);
       if (!list.needed(list.entry(it), wave)) continue;
       const int j0 = list.tile(list.entry(it)) * kRuleTile;
@@ -222,10 +226,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
   for (int it = 0; it < total; ++it) {
     __syncthreads();
     if (tid < kRuleTile) { docs[tid] = RuleRows::q_id(rd); docs[kRuleTile + tid] = rlim; ls[tid] = rd >= 0 ? rule_lse2(rl) : INFINITY; ls[kRuleTile + tid] = rdl; }
-    __syncthreads();
-    rule_store<A>(xs, tid, rx, docs);
-    rule_store<A>(ys, tid, ry, docs);
-    __syncthreads();
+    rule_stage<A>(list.plain(list.entry(it % n)), xs, rx, ys, ry, tid, docs);
     if (it + 1 < total) load(it + 1);
     const int item = it % n;
     if (!list.needed(list.entry(item), wave)) continue;
