@@ -8,6 +8,8 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
+import threading
 
 import numpy as np
 
@@ -177,11 +179,6 @@ def _refuse(what: str):
     raise PtError(PT_EINVAL, what)
 
 
-def _op_chk(lib, st):
-    if st != PT_OK:
-        raise PtError(st, (lib.pt_last_error(None) or b"").decode())
-
-
 def _dtype_of(t) -> int:
     if not _DTYPES:
         _op_setup()
@@ -200,21 +197,56 @@ def _device_of(first, *others) -> int:
     return at
 
 
+class _Args(threading.local):
+    """Room for the structs of one call of this thread, filled in one go: a pt_attention and up to eight pt_heads behind it.  (A
+    call reads them before it returns; making ten ctypes objects takes longer than a short kernel.)"""
+
+    def __init__(self):
+        self.buf = C.create_string_buffer(80 + 8 * 32)
+        self.at = C.addressof(self.buf)
+        self.heads = [self.at + 80 + 32 * i for i in range(8)]
+
+
+_args = _Args()
+_PACK = {n: struct.Struct("9i2f4x4Q" + n * "Qqqq").pack_into for n in (4, 8)}
+
+
+def _fast_library():
+    """The library with pointers taken as plain addresses."""
+    global _fast
+    load_library()
+    lib = C.CDLL(LIB_PATH)
+    vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
+    lib.pt_attention_fwd.argtypes = [vp] * 7
+    lib.pt_attention_bwd.argtypes = [vp] * 11 + [sz, vp]
+    lib.pt_gelu8_fwd.argtypes = [i32, vp, vp, vp, vp, i64, i32, vp]
+    lib.pt_gelu8_bwd.argtypes = [i32, vp, vp, vp, vp, vp, i64, i32, vp]
+    _fast = lib
+    return lib
+
+
+_fast = None
+
+
 def _launch(at: int, call, *args):
     """call(*args, current stream of GPU `at`), with that GPU as the current one."""
     if at == _torch.cuda.current_device():
-        return call(*args, _torch._C._cuda_getCurrentRawStream(at))
-    with _torch.cuda.device(at):
-        return call(*args, _torch._C._cuda_getCurrentRawStream(at))
+        st = call(*args, _torch._C._cuda_getCurrentRawStream(at))
+    else:
+        with _torch.cuda.device(at):
+            st = call(*args, _torch._C._cuda_getCurrentRawStream(at))
+    if st != PT_OK:
+        raise PtError(st, (load_library().pt_last_error(None) or b"").decode())
 
 
-def _heads(t, name: str, shape, dtype) -> PtHeads:
+def _heads(t, name: str, shape, dtype) -> tuple:
+    """The four fields of a pt_heads."""
     if t.shape != shape or t.dtype is not dtype:
         _refuse(f"{name}: {t.dtype} {tuple(t.shape)}, not {dtype} {tuple(shape)}")
     a, b, c, d = t.stride()
     if d != 1 and t.numel() > 0:
         _refuse(f"{name}: the head size must be contiguous")
-    return PtHeads(t.data_ptr(), a, b, c)
+    return t.data_ptr(), a, b, c
 
 
 def _plain(t, dtype, shape, name: str):
@@ -238,30 +270,38 @@ class AttentionRule:
     def __init__(self, order="full", scale=None, cap=0.0, slopes=None, documents=None, q_documents=None, prefix=None, q0=0):
         if order not in ATTN_ORDERS:
             _refuse(f"order {order!r}: one of {', '.join(ATTN_ORDERS)}")
+        if not 0 <= q0 < 1 << 24 or not 0.0 <= cap <= 3e38 or not (scale is None or 0.0 < scale <= 3e38):
+            _refuse(f"q0 {q0}, cap {cap}, scale {scale}: q0 in 0 .. 2^24, cap not negative, scale positive")
         self.order, self.scale, self.cap, self.q0 = order, scale, cap, q0
         self.slopes, self.documents, self.prefix = slopes, documents, prefix
         self.q_documents = documents if q_documents is None else q_documents
         if self.q_documents is not None and documents is None:
             _refuse("documents of the queries and of the keys go together")
 
-    def describe(self, q, k) -> PtAttention:
+    def _fields(self, q, k) -> tuple:
+        """The fields of pt_attention for these tensors."""
         if q.dim() != 4 or k.dim() != 4:
             _refuse("q, k and v: [samples, rows, heads, head size]")
         nb, Sq, H, dh = q.shape
-        Sk, Hkv = k.shape[1:3]
+        kb, Sk, Hkv, kd = k.shape
+        if kb != nb or kd != dh:
+            _refuse(f"q {tuple(q.shape)} and k {tuple(k.shape)} differ in samples or head size")
         dtype = _dtype_of(q)
-        a = PtAttention(dtype, nb, Sq, Sk, H, Hkv, dh, ATTN_ORDERS[self.order], self.q0,
-                        (dh ** -0.5 if dh else 1.0) if self.scale is None else self.scale, self.cap)
+        slopes = qd = kdoc = prefix = 0
         if self.slopes is not None:
-            a.slopes = _plain(self.slopes, _torch.float32, (H,), "slopes")
+            slopes = _plain(self.slopes, _torch.float32, (H,), "slopes")
         if self.documents is not None:
-            a.k_documents = _plain(self.documents, _torch.int32, (nb, Sk), "documents")
-            a.q_documents = _plain(self.q_documents, _torch.int32, (nb, Sq), "q_documents")
+            kdoc = _plain(self.documents, _torch.int32, (nb, Sk), "documents")
+            qd = kdoc if self.q_documents is self.documents and Sq == Sk else _plain(self.q_documents, _torch.int32, (nb, Sq), "q_documents")
         if self.order == "prefix":
             if self.prefix is None:
                 _refuse("order \"prefix\" needs prefix lengths")
-            a.prefix = _plain(self.prefix, _torch.int32, (nb,), "prefix")
-        return a
+            prefix = _plain(self.prefix, _torch.int32, (nb,), "prefix")
+        return (dtype, nb, Sq, Sk, H, Hkv, dh, ATTN_ORDERS[self.order], self.q0,
+                (dh ** -0.5 if dh else 1.0) if self.scale is None else self.scale, self.cap, slopes, qd, kdoc, prefix)
+
+    def describe(self, q, k) -> PtAttention:
+        return PtAttention(*self._fields(q, k))
 
 
 _FULL = AttentionRule()
@@ -271,41 +311,42 @@ def attention_forward(q, k, v, rule: AttentionRule | None = None, out=None, want
     """(o, lse): q [nb, Sq, H, dh], k and v [nb, Sk, Hkv, dh], views of any strides that are multiples of 16 bytes; o like q, lse
     float32 [nb, H, Sq] (None if not wanted)."""
     rule = rule or _FULL
-    a = rule.describe(q, k)
+    a = rule._fields(q, k)
     qs, ks, dtype = q.shape, k.shape, q.dtype
-    if ks[0] != qs[0] or ks[3] != qs[3]:
-        _refuse(f"q {tuple(qs)} and k {tuple(ks)} differ in samples or head size")
     hq, hk, hv = _heads(q, "q", qs, dtype), _heads(k, "k", ks, dtype), _heads(v, "v", ks, dtype)
     at = _device_of(q, k, v, out, rule.slopes, rule.documents, rule.q_documents, rule.prefix)
-    o = _torch.empty(qs, dtype=dtype, device=q.device) if out is None else out
-    lse = _torch.empty((qs[0], qs[2], qs[1]), dtype=_torch.float32, device=q.device) if want_lse else None
-    lib = _lib or load_library()
-    _op_chk(lib, _launch(at, lib.pt_attention_fwd, a, hq, hk, hv, _heads(o, "out", qs, dtype), lse.data_ptr() if want_lse else None))
+    _, nb, Sq, _, H, _, dh = a[:7]
+    o = _torch.empty_like(q, memory_format=_torch.contiguous_format) if out is None else out
+    lse = _torch.empty((nb, H, Sq), dtype=_torch.float32, device=q.device) if want_lse else None
+    lib, args = _fast or _fast_library(), _args
+    _PACK[4](args.buf, 0, *a, *hq, *hk, *hv, *((o.data_ptr(), Sq * H * dh, H * dh, dh) if out is None else _heads(o, "out", qs, dtype)))
+    _launch(at, lib.pt_attention_fwd, args.at, *args.heads[:4], lse.data_ptr() if want_lse else None)
     return o, lse
 
 
 def attention_backward(q, k, v, o, lse, do, rule: AttentionRule | None = None, grads=None):
     """(dq, dk, dv) of the call that returned (o, lse); grads: tensors (views) to write them to."""
     rule = rule or _FULL
-    a = rule.describe(q, k)
+    a = rule._fields(q, k)
     qs, ks, dtype = q.shape, k.shape, q.dtype
-    if ks[0] != qs[0] or ks[3] != qs[3]:
-        _refuse(f"q {tuple(qs)} and k {tuple(ks)} differ in samples or head size")
-    views = (_heads(q, "q", qs, dtype), _heads(k, "k", ks, dtype), _heads(v, "v", ks, dtype), _heads(o, "o", qs, dtype))
-    stats = _plain(lse, _torch.float32, (qs[0], qs[2], qs[1]), "lse")
-    hd = _heads(do, "do", qs, dtype)
+    _, nb, Sq, Sk, H, Hkv, dh = a[:7]
+    hq, hk, hv = _heads(q, "q", qs, dtype), _heads(k, "k", ks, dtype), _heads(v, "v", ks, dtype)
+    ho, hd = _heads(o, "o", qs, dtype), _heads(do, "do", qs, dtype)
+    stats = _plain(lse, _torch.float32, (nb, H, Sq), "lse")
     at = _device_of(q, k, v, o, lse, do, rule.slopes, rule.documents, rule.q_documents, rule.prefix, *(grads or ()))
     if grads is None:
-        dq = _torch.empty(qs, dtype=dtype, device=q.device)
-        dk = _torch.empty(ks, dtype=dtype, device=q.device)
-        dv = _torch.empty(ks, dtype=dtype, device=q.device)
+        dense = _torch.contiguous_format
+        dq, dk, dv = _torch.empty_like(q, memory_format=dense), _torch.empty_like(k, memory_format=dense), _torch.empty_like(k, memory_format=dense)
+        rq, rk = (Sq * H * dh, H * dh, dh), (Sk * Hkv * dh, Hkv * dh, dh)
+        out = (dq.data_ptr(), *rq, dk.data_ptr(), *rk, dv.data_ptr(), *rk)
     else:
         dq, dk, dv = grads
-    lib, need = _lib or load_library(), C.c_size_t()
-    _op_chk(lib, lib.pt_attention_workspace(a, need))
-    ws = _torch.empty((need.value,), dtype=_torch.uint8, device=q.device)
-    _op_chk(lib, _launch(at, lib.pt_attention_bwd, a, *views, stats, hd, _heads(dq, "dq", qs, dtype), _heads(dk, "dk", ks, dtype),
-                         _heads(dv, "dv", ks, dtype), ws.data_ptr(), need.value))
+        out = (*_heads(dq, "dq", qs, dtype), *_heads(dk, "dk", ks, dtype), *_heads(dv, "dv", ks, dtype))
+    lib, args = _fast or _fast_library(), _args
+    _PACK[8](args.buf, 0, *a, *hq, *hk, *hv, *ho, *hd, *out)
+    ws = _torch.empty_like(lse)      # as many bytes as pt_attention_workspace asks for, which the call checks
+    h = args.heads
+    _launch(at, lib.pt_attention_bwd, args.at, h[0], h[1], h[2], h[3], stats, h[4], h[5], h[6], h[7], ws.data_ptr(), 4 * nb * H * Sq)
     return dq, dk, dv
 
 
@@ -316,11 +357,11 @@ def gelu8_forward(h):
         _refuse("h: [rows, F], contiguous")
     T, F = h.shape
     at, dev = _device_of(h), h.device
-    g = _torch.empty((T, F), dtype=h.dtype, device=dev)
+    g = _torch.empty_like(h)
     codes = _torch.empty((T, F), dtype=_torch.int8, device=dev)
     exps = _torch.empty((T, (F + 31) // 32), dtype=_torch.uint8, device=dev)
-    lib = _lib or load_library()
-    _op_chk(lib, _launch(at, lib.pt_gelu8_fwd, dtype, h.data_ptr(), g.data_ptr(), codes.data_ptr(), exps.data_ptr(), T, F))
+    lib = _fast or _fast_library()
+    _launch(at, lib.pt_gelu8_fwd, dtype, h.data_ptr(), g.data_ptr(), codes.data_ptr(), exps.data_ptr(), T, F)
     return g, codes, exps
 
 
@@ -333,11 +374,11 @@ def gelu8_backward(codes, exps, dg, want_activation: bool = True, out=None):
     pc = _plain(codes, _torch.int8, (T, F), "codes")
     pe = _plain(exps, _torch.uint8, (T, (F + 31) // 32), "exps")
     at = _device_of(dg, codes, exps, out)
-    dh = _torch.empty((T, F), dtype=dg.dtype, device=dg.device) if out is None else out
+    dh = _torch.empty_like(dg) if out is None else out
     pd = dh.data_ptr() if out is None else _plain(out, dg.dtype, (T, F), "out")
-    g = _torch.empty((T, F), dtype=dg.dtype, device=dg.device) if want_activation else None
-    lib = _lib or load_library()
-    _op_chk(lib, _launch(at, lib.pt_gelu8_bwd, dtype, pc, pe, dg.data_ptr(), pd, g.data_ptr() if want_activation else None, T, F))
+    g = _torch.empty_like(dg) if want_activation else None
+    lib = _fast or _fast_library()
+    _launch(at, lib.pt_gelu8_bwd, dtype, pc, pe, dg.data_ptr(), pd, g.data_ptr() if want_activation else None, T, F)
     return dh, g
 
 

@@ -157,7 +157,17 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
     const float* vp = static_cast<const float*>(g.v.p) + b * g.v.b + hk * g.v.h;
     const ScoreF sc(g, h);
     const float lw = on ? rule_lse2(g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i]) : INFINITY;
-    const float dl = on ? g.delta[((int64_t)b * g.H + h) * g.Sq + i] : 0.f;
+    float dl = 0.f;   // delta = dO . o
+    {
+      f32x4 o[A::NF];
+      A::own(static_cast<const float*>(g.o.p) + b * g.o.b + h * g.o.h, g.o.t, on ? i : g.Sq, g.Sq, g.dh, gr, 1.f, o);
+#pragma unroll
+      for (int x = 0; x < A::NF; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dl = fmaf(a1[x][e], o[x][e], dl);
+      dl += __shfl_xor(dl, 16, 64);
+      dl += __shfl_xor(dl, 32, 64);
+    }
     int rd = 0;
     auto load = [&](int it) {
       const int j0 = list.tile(list.entry(it)) * kRuleTile;
@@ -204,28 +214,39 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
   const int n = list.build<false>(g, rows, wave, lane, u.blk, kd, ok);
   A::own(static_cast<const float*>(g.k.p) + b * g.k.b + hk * g.k.h, g.k.t, on ? j : g.Sk, g.Sk, g.dh, gr, 1.f, a0);
   A::own(static_cast<const float*>(g.v.p) + b * g.v.b + hk * g.v.h, g.v.t, on ? j : g.Sk, g.Sk, g.dh, gr, 1.f, a1);
-  f32x4 ay[A::NF];
+  f32x4 ay[A::NF], ro[A::N4];
 #pragma unroll
   for (int x = 0; x < A::NF; ++x) ay[x] = f32x4{0.f, 0.f, 0.f, 0.f};
   int rd = 0, rlim = 0;
-  float rl = 0.f, rdl = 0.f;
+  float rl = 0.f;
   auto load = [&](int it) {
     const int h = hk * G + it / n, i0 = list.tile(list.entry(it % n)) * kRuleTile;
     A::load(static_cast<const float*>(g.q.p) + b * g.q.b + h * g.q.h, g.q.t, i0, g.Sq, g.dh, tid, rx);
     A::load(static_cast<const float*>(g.d_o.p) + b * g.d_o.b + h * g.d_o.h, g.d_o.t, i0, g.Sq, g.dh, tid, ry);
+    A::load(static_cast<const float*>(g.o.p) + b * g.o.b + h * g.o.h, g.o.t, i0, g.Sq, g.dh, tid, ro);
     if (tid < kRuleTile) {
       const int i = i0 + tid;
       rd = rows.q_raw(g, i);
       rlim = rows.lim(g, i);
       rl = i < g.Sq ? g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i] : -INFINITY;
-      rdl = i < g.Sq ? g.delta[((int64_t)b * g.H + h) * g.Sq + i] : 0.f;
     }
   };
   const int total = n * G;
   if (total > 0) load(0);
   for (int it = 0; it < total; ++it) {
     __syncthreads();
-    if (tid < kRuleTile) { docs[tid] = RuleRows::q_id(rd); docs[kRuleTile + tid] = rlim; ls[tid] = rd >= 0 ? rule_lse2(rl) : INFINITY; ls[kRuleTile + tid] = rdl; }
+    if (tid < kRuleTile) { docs[tid] = RuleRows::q_id(rd); docs[kRuleTile + tid] = rlim; ls[tid] = rd >= 0 ? rule_lse2(rl) : INFINITY; }
+#pragma unroll
+    for (int x = 0; x < A::N4; ++x) {   // delta of the tile's rows: DP / 4 neighbouring lanes hold a row
+      int r, d;
+      A::place(tid, x, &r, &d);
+      float part = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) part = fmaf(ry[x][e], ro[x][e], part);
+#pragma unroll
+      for (int o = 1; o < DP / 4; o <<= 1) part += __shfl_xor(part, o, 64);
+      if (d == 0) ls[kRuleTile + r] = part;
+    }
     rule_stage<A>(list.plain(list.entry(it % n)), xs, rx, ys, ry, tid, docs);
     if (it + 1 < total) load(it + 1);
     const int item = it % n;
@@ -255,28 +276,6 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_bwd_f32_kernel(Attn
   }
 }
 
-// delta[b, h, i] = dO . o of one query and head, 0 for padding (whose rows may hold anything).  16 lanes a row; rows are taken
-// with the heads next to each other, as a packed layout has them.
-__global__ __launch_bounds__(256) void rule_delta_kernel(AttnRuleArgs g) {
-  const int64_t r = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), total = (int64_t)g.nb * g.Sq * g.H;
-  if (r >= total) return;
-  const int h = (int)(r % g.H), l = threadIdx.x & 15;
-  const int64_t t = r / g.H;
-  const int i = (int)(t % g.Sq), b = (int)(t / g.Sq);
-  const RuleRows rows(g, b);
-  const float* o = static_cast<const float*>(g.o.p) + b * g.o.b + (int64_t)i * g.o.t + h * g.o.h;
-  const float* d = static_cast<const float*>(g.d_o.p) + b * g.d_o.b + (int64_t)i * g.d_o.t + h * g.d_o.h;
-  float s = 0.f;
-  for (int c = 4 * l; c < g.dh; c += 64) {
-    const f32x4 a = load4(o + c), e = load4(d + c);
-#pragma unroll
-    for (int x = 0; x < 4; ++x) s = fmaf(a[x], e[x], s);
-  }
-#pragma unroll
-  for (int x = 1; x < 16; x <<= 1) s += __shfl_xor(s, x, 64);
-  if (l == 0) g.delta[((int64_t)b * g.H + h) * g.Sq + i] = rows.qdoc(g, i) >= 0 ? s : 0.f;
-}
-
 template <int DP>
 hipError_t launch_f32(const AttnRuleArgs& g, bool bwd, hipStream_t st) {
   const int nt = ((bwd && g.Sq > g.Sk ? g.Sq : g.Sk) + kRuleTile - 1) / kRuleTile;
@@ -293,11 +292,6 @@ hipError_t launch_f32(const AttnRuleArgs& g, bool bwd, hipStream_t st) {
 }  // namespace
 
 hipError_t attention_rule_f32(const AttnRuleArgs& g, bool bwd, hipStream_t st) {
-  if (bwd && g.Sq > 0 && g.nb > 0) {   // (without queries the launch below writes zeros)
-    hipLaunchKernelGGL(rule_delta_kernel, dim3((unsigned)(((int64_t)g.nb * g.Sq * g.H + 15) / 16)), dim3(256), 0, st, g);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
   if (g.dh <= 16) return launch_f32<16>(g, bwd, st);
   if (g.dh <= 32) return launch_f32<32>(g, bwd, st);
   if (g.dh <= 64) return launch_f32<64>(g, bwd, st);

@@ -88,7 +88,7 @@ pt_status pt_attention_workspace(const pt_attention* a, size_t* bwd_bytes) {
   const pt_status s = check_attention(a);
   if (s != PT_OK) return s;
   if (!bwd_bytes) return fail(PT_EINVAL, "bwd_bytes is NULL");
-  *bwd_bytes = (size_t)a->nb * a->H * a->Sq * sizeof(float);
+  *bwd_bytes = a->dtype == PT_BF16 ? (size_t)a->nb * a->H * a->Sq * sizeof(float) : 0;   // delta, which the fp32 kernels keep to themselves
   return PT_OK;
 }
 
