@@ -75,13 +75,13 @@ __device__ __forceinline__ int rule_wave_min(int v) {
 }
 __device__ __forceinline__ int rule_wave_max(int v) { return ~rule_wave_min(~v); }
 
-// The tiles that a workgroup of four waves visits, each wave owning ROWS rows: entries tile << 9 | plain << 8 | whole bits << 4 |
+// The tiles that a workgroup of four waves visits, SHARE waves owning ROWS rows together: entries tile << 9 | plain << 8 | whole bits << 4 |
 // needed bits.  plain: all its rows exist and none is padding.
 // In LDS: the least and the largest document of each wave's rows and of each tile (the sign of the least says that padding is among
 // them, that of the largest that padding or several documents are), then, in place of the tiles' least, the entries.  A tile is needed by a wave whose range of
 // documents meets its own and whose positions reach it; it is whole if both are one and the same document and all positions of
 // the wave see all of the tile.
-template <int ROWS>
+template <int ROWS, int SHARE = 1>
 struct RuleList {
   int* base;
   int tiles;
@@ -138,7 +138,7 @@ struct RuleList {
         int e = 0;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          const int o0 = (blk * 4 + w) * ROWS, o1 = o0 + ROWS - 1 < m ? o0 + ROWS - 1 : m - 1;
+          const int o0 = (blk * (4 / SHARE) + w / SHARE) * ROWS, o1 = o0 + ROWS - 1 < m ? o0 + ROWS - 1 : m - 1;
           const int wlo = docs ? base[2 * w] & 0x7fffffff : 0, whi_ = docs ? base[2 * w + 1] : 0, whi = whi_ & 0x7fffffff;
           bool need = t < tiles && o0 < m && tlo <= whi && wlo <= thi;
           bool all = thi_ >= 0 && whi_ >= 0 && tlo == wlo;

@@ -57,8 +57,7 @@ pt_status check_attention(const pt_attention* a) {
   if (!(a->cap >= 0.f) || !std::isfinite(a->cap * 3.f) || (a->cap > 0.f && !std::isfinite(a->scale * 3.f / a->cap))) return fail(PT_EINVAL, "cap must be 0 or a positive finite number");
   // one launch covers the owned blocks of 64 rows of both passes
   const int64_t blocks = (int64_t)a->nb * a->H * ((a->Sq + 63) / 64) + (int64_t)a->nb * a->Hkv * ((a->Sk + 63) / 64);
-  const int64_t rows = ((int64_t)a->nb * a->Sq * a->H + 15) / 16;
-  if (blocks >= (1 << 24) || rows >= (1 << 24)) return fail(PT_EINVAL, "nb * H * Sq or nb * Hkv * Sk too large");
+  if (blocks >= (1 << 24)) return fail(PT_EINVAL, "nb * H * Sq or nb * Hkv * Sk too large");
   return PT_OK;
 }
 AttnRuleArgs rule_args(const pt_attention* a) {

@@ -155,9 +155,29 @@ def test_documents_far_apart_in_a_long_row():
     compare(q, k, v, do, docs)
 
 
-def test_results_repeat_bit_for_bit_on_any_stream_and_in_a_graph():
+def test_the_longest_row():
+    """2^18 keys, 4096 tiles: a few queries at its end, a document that starts where the row does and one that ends there."""
+    gen = torch.Generator().manual_seed(12)
+    Sk, Sq = 1 << 18, 40
+    q, k, v, do = inputs(1, Sq, Sk, 1, 1, 16, BF16, gen)
+    docs = torch.zeros(1, Sk, dtype=torch.int32)
+    docs[0, 100000:] = 1
+    q_docs = torch.ones(1, Sq, dtype=torch.int32)
+    q_docs[0, :7] = 0
+    compare(q, k, v, do, docs, q_docs, order="causal", q0=Sk - Sq)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_more_workgroups_than_the_gpu_has_cus(dtype):
+    gen = torch.Generator().manual_seed(13)
+    q, k, v, do = inputs(8, 260, 260, 8, 8, 32, dtype, gen)
+    compare(q, k, v, do, documents("packed", 8, 260, gen), order="prefix", prefix=torch.arange(8, dtype=torch.int32) * 30, cap=12.0)
+
+
+@pytest.mark.parametrize("dtype,dh", [(BF16, 64), (BF16, 128), (F32, 128)], ids=["bf16 64", "bf16 128", "f32 128"])
+def test_results_repeat_bit_for_bit_on_any_stream_and_in_a_graph(dtype, dh):
     gen = torch.Generator().manual_seed(10)
-    q, k, v, do = inputs(4, 300, 300, 4, 2, 64, BF16, gen)
+    q, k, v, do = inputs(4, 300, 300, 4, 2, dh, dtype, gen)
     docs = documents("packed", 4, 300, gen)
     first = both(q, k, v, do, docs, cap=10.0)
     side = torch.cuda.Stream()
@@ -172,7 +192,7 @@ def test_results_repeat_bit_for_bit_on_any_stream_and_in_a_graph():
         o, lse = binding.attention_forward(q, k, v, rule)
         grads = binding.attention_backward(q, k, v, o, lse, do, rule)
     for step in range(3):
-        q.copy_((torch.randn(q.shape, generator=gen)).to(BF16))
+        q.copy_((torch.randn(q.shape, generator=gen)).to(dtype))
         graph.replay()
         torch.cuda.synchronize()
         want = both(q, k, v, do, docs, cap=10.0)
