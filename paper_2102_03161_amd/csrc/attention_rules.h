@@ -147,7 +147,7 @@ struct RuleList {
             all = all && r1 <= rows.lim(g, o0);
           } else {
             need = need && lim1 >= o0;
-            all = all && lim0 >= o1;
+            all = all && lim0 >= o1 && o0 + ROWS <= m;   // (fewer keys: a query may see one only, which whole tiles rule out)
           }
           e |= (need ? 1 : 0) << w | (need && all ? 1 : 0) << (4 + w);
         }

@@ -402,8 +402,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
 // of the weight, is as large as dS itself.  So the pass uses that value d only to centre dP, and takes out what is left of it:
 // with r_i = sum_j p_ij (dP_ij - d_i), the true delta is d_i + r_i, and dq_i = scale (sum_j w_ij (dP_ij - d_i) k_j - r_i sum_j
 // w_ij k_j), w = p (1 - tanh^2): one more product with the keys' fragments that the pass has in registers anyway.  Without a cap
-// r is summed from dS as rounded to bf16 for the product, two to an instruction: the part of those roundings that all keys share,
-// which dS itself, summing to 0, does not have, then cancels.
+// the r of that product is summed from dS as it was rounded to bf16 for the other (two to an instruction): the part of those
+// roundings that all keys share, which dS itself, summing to 0, does not have, then cancels.
 // p of 1 means a query that sees one key: dS is exactly 0 then, where dP - delta would leave the rounding of two different sums
 // (for dq the correction below comes to exactly 0 by itself, but with a cap)
 constexpr float kOneKey = 1.f - 1.f / 65536.f;
@@ -435,7 +435,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 1) void rule_dq_kernel(AttnRule
   f32x16 dq[T::DT], wk[T::DT];
 #pragma unroll
   for (int dt = 0; dt < T::DT; ++dt) { dq[dt] = zero16(); wk[dt] = zero16(); }
-  float rest = 0.f;
+  float rest = 0.f, rounded = 0.f;   // r, and r from dS as it was rounded
   auto load = [&](int e, int at) {
     const int j0 = list.tile(e) * kRuleTile;
     sd.load(j0);
@@ -489,14 +489,14 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 1) void rule_dq_kernel(AttnRule
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
           dp[v] *= w[v];
+          rest += dp[v];
           if (MOD & 1) {
-            rest += dp[v];
             const float f = 4.f * s[v] * (1.f - s[v]);
             dp[v] *= f;
             w[v] *= f;
           }
         }
-        T::add2(T::col_addr(kb, lane), 32 * st, dp, dq, w, wk, (MOD & 1) ? nullptr : &rest);
+        T::add2(T::col_addr(kb, lane), 32 * st, dp, dq, w, wk, (MOD & 1) ? nullptr : &rounded);
       }
     }
     if (it + 1 < n) finish(next, (it + 1) & 1);
@@ -504,12 +504,13 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 1) void rule_dq_kernel(AttnRule
     next = list.entry(it + 2 <= list.tiles ? it + 2 : list.tiles);
   }
   rest += half_swap(rest);
+  rounded = (MOD & 1) ? rest : rounded + half_swap(rounded);
   if (!ok) return;
   if (half == 0) g.delta[((int64_t)b * g.H + h) * g.Sq + i] = on ? dl + rest : 0.f;
 #pragma unroll
   for (int dt = 0; dt < T::DT; ++dt)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) dq[dt][v] = fmaf(-rest, wk[dt][v], dq[dt][v]);
+    for (int v = 0; v < 16; ++v) dq[dt][v] = fmaf(-rounded, wk[dt][v], dq[dt][v]);
   T::put(static_cast<bf16*>(const_cast<void*>(g.dq.p)) + b * g.dq.b + (int64_t)i * g.dq.t + h * g.dq.h, g.dh, half, g.scale, dq);
 }
 

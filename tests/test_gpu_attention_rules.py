@@ -107,14 +107,27 @@ def test_padding_may_hold_anything_and_gets_zeros(dtype):
     assert torch.isinf(got["lse"].transpose(1, 2)[pad]).all()
 
 
+@pytest.mark.parametrize("cap,slopes", [(0.0, False), (15.0, False), (50.0, True), (0.0, True)])
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
-def test_a_query_that_sees_one_key_copies_its_value_and_has_no_gradient(dtype):
+def test_a_query_that_sees_one_key_copies_its_value_and_has_no_gradient(dtype, cap, slopes):
     gen = torch.Generator().manual_seed(6)
-    for S, docs in ((1, None), (70, torch.arange(70, dtype=torch.int32).view(1, -1))):
-        q, k, v, do = inputs(1, S, S, 2, 2, 64, dtype, gen)
-        got = both(q, k, v, do, docs)
-        assert torch.equal(got["o"], v) and torch.equal(got["dv"], do)
+    rule = dict(cap=cap, slopes=torch.tensor([0.1, 0.4]) if slopes else None)
+    for nb, S, docs in ((50, 1, None), (1, 70, torch.arange(70, dtype=torch.int32).view(1, -1))):
+        q, k, v, do = inputs(nb, S, S, 2, 2, 64, dtype, gen)
+        got = both(q, k, v, do, docs, **rule)
+        assert torch.equal(got["o"], v)
+        # the probability itself comes from the row's statistic again: e^(s - lse), where s and lse, of size up to cap (or 12 without
+        # one), are each a few fp32 roundings (16 of cap + |s| for the capped score, 8 of |lse|); bf16 rounds that away
+        off = 0.0 if dtype == BF16 else 2.0 ** -24 * (2 * 16 * 2 * (cap or 12.0) + 8 * (cap or 12.0))
+        assert ((got["dv"] - do).abs() <= off * do.abs()).all()
         assert not got["dq"].any() and not got["dk"].any()
+    # the last key alone in its document, seen by a tile of queries that see nothing else
+    q, k, v, do = inputs(1, 64, 33, 2, 2, 64, dtype, gen)
+    docs = torch.zeros(1, 33, dtype=torch.int32)
+    docs[0, 32] = 1
+    got = both(q, k, v, do, docs, torch.ones(1, 64, dtype=torch.int32), **rule)
+    assert torch.equal(got["o"], v[:, 32:].expand(1, 64, 2, 64))
+    assert not got["dq"].any() and not got["dk"].any()
 
 
 def test_views_of_any_strides_and_broadcast_keys():
