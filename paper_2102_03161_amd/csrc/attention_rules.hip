@@ -271,28 +271,54 @@ __device__ __forceinline__ void four(const int* p, int (&x)[4]) {
 // ---------------------------------------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------------------------------------
+// Two waves that share their rows: the second one's accumulators through LDS (both buffers' tiles, which nothing reads any more),
+// 16 bytes a lane next to each other.
+template <int N>
+__device__ __forceinline__ void leave(float* room, int group, int lane, const f32x16 (&acc)[N]) {
+#pragma unroll
+  for (int i = 0; i < 4 * N; ++i) {
+    const f32x16& a = acc[i >> 2];
+    const int v = 4 * (i & 3);
+    *reinterpret_cast<float4*>(room + ((group * 4 * N + i) * 64 + lane) * 4) = make_float4(a[v], a[v + 1], a[v + 2], a[v + 3]);
+  }
+}
+template <int N>
+__device__ __forceinline__ void take(const float* room, int group, int lane, f32x16 (&acc)[N], float f, float f2) {
+#pragma unroll
+  for (int i = 0; i < 4 * N; ++i) {
+    const float4 x = *reinterpret_cast<const float4*>(room + ((group * 4 * N + i) * 64 + lane) * 4);
+    const float e[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      acc[i >> 2][4 * (i & 3) + v] = acc[i >> 2][4 * (i & 3) + v] * f + e[v] * f2;
+    }
+  }
+}
+
 // A row's reference m (log2 domain) only has to keep exp2 in range: it is the maximum of the first tile in which the row sees
 // anything, and moves only when a tile's sum passes 2^40.  So a tile whose rows all have one needs no maximum at all.
 constexpr float kGrown = 1099511627776.f;   // 2^40
 
-template <int DP, int MOD>
+template <int DP, int MOD, int SHARE>
 __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
+  constexpr int kRows = 128 / SHARE, NX = 2 / SHARE;   // rows of a workgroup; parts of 32 rows of a tile that a wave takes
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   int* kdoc = reinterpret_cast<int*>(smem + 4 * T::BYTES);                    // [2][64], behind [2][K tile, V tile]
-  const RuleList<32> list(kdoc + 2 * kRuleTile, g.Sk);
+  const RuleList<32, SHARE> list(kdoc + 2 * kRuleTile, g.Sk);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  const int nqb = (g.Sq + 127) / 128;
+  const int group = wave / SHARE, x0 = wave % SHARE * NX;   // rows of the wave; its first part of a tile
+  const int nqb = (g.Sq + kRows - 1) / kRows;
   const RuleUnit u(g, nqb, g.H, blockIdx.x, gridDim.x, g.order != 0);
   const int b = u.b, h = u.h, hk = h / (g.H / g.Hkv);
-  const int i = u.blk * 128 + wave * 32 + (lane & 31);
+  const int i = u.blk * kRows + group * 32 + (lane & 31);
   const RuleRows rows(g, b);
   const bool ok = i < g.Sq;
   const int lim = rows.lim(g, i), qd = rows.qdoc(g, i);
   const bool on = ok && qd >= 0;
   bf16x8 qf[T::KS];
   T::own(static_cast<const bf16*>(g.q.p) + b * g.q.b + (int64_t)i * g.q.t + h * g.q.h, on, g.dh, half, qf);
-  const int n = list.build<true>(g, rows, wave, lane, u.blk, qd, ok);
+  const int n = list.template build<true>(g, rows, wave, lane, u.blk, qd, ok);
   const Streams<DP> kv(g.k, hk, g.v, hk, b, wave, lane);
   StreamDocs<DP> sd(rows.k, g.Sk, kv.row);
   const unsigned lds = lds_addr(smem), mine = lds + wave * T::N * 1024;
@@ -321,24 +347,24 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
     if (list.needed(e, wave)) {
       const unsigned kb = lds + (it & 1) * 2 * T::BYTES;
       const int j0 = list.tile(e) * kRuleTile;
-      const float at = (float)(g.q0 + i - j0 - 4 * half);
-      f32x16 s[2];
+      const float at = (float)(g.q0 + i - j0 - 32 * x0 - 4 * half);
+      f32x16 s[NX];
       // scores less the reference, of the visible pairs; -infinity of the others
       auto scores = [&]() {
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          s[st] = T::dot(T::row_addr(kb, lane), 32 * st, qf);
+        for (int st = 0; st < NX; ++st) {
+          s[st] = T::dot(T::row_addr(kb, lane) + 32 * x0 * T::RB, 32 * st, qf);
 #pragma unroll
           for (int v = 0; v < 16; ++v) s[st][v] = sc.at<MOD>((MOD & 1) ? sc.bend(s[st][v]) : s[st][v], at - (float)(32 * st + acc_row(v)), -m);
         }
         if (!list.whole(e, wave)) {
-          const int far = lim - j0 - 4 * half;
+          const int far = lim - j0 - 32 * x0 - 4 * half;
 #pragma unroll
-          for (int st = 0; st < 2; ++st)
+          for (int st = 0; st < NX; ++st)
 #pragma unroll
             for (int g4 = 0; g4 < 4; ++g4) {
               int kd[4];
-              four(kdoc + (it & 1) * kRuleTile + 32 * st + 8 * g4 + 4 * half, kd);
+              four(kdoc + (it & 1) * kRuleTile + 32 * (x0 + st) + 8 * g4 + 4 * half, kd);
 #pragma unroll
               for (int x = 0; x < 4; ++x) s[st][4 * g4 + x] = kd[x] == qd ? s[st][4 * g4 + x] : -INFINITY;
               if (g.order != 0) {   // (rows behind the last have no document)
@@ -351,7 +377,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
       auto weights = [&](float shift) {
         float sum = 0.f;
 #pragma unroll
-        for (int st = 0; st < 2; ++st)
+        for (int st = 0; st < NX; ++st)
 #pragma unroll
           for (int v = 0; v < 16; ++v) {
             s[st][v] = fast_exp2(s[st][v] - shift);
@@ -370,7 +396,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
         scores();
         float mx = s[0][0];
 #pragma unroll
-        for (int v = 1; v < 32; ++v) mx = fmaxf(mx, s[v >> 4][v & 15]);
+        for (int v = 1; v < 16 * NX; ++v) mx = fmaxf(mx, s[v >> 4][v & 15]);
         mx = fmaxf(mx, half_swap(mx));
         const bool move = mx > -INFINITY && (lsum == 0.f || mx > 0.f);
         const float up = move ? mx : 0.f, alpha = fast_exp2(-up);
@@ -384,11 +410,29 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
       }
       lsum += sum + half_swap(sum);
 #pragma unroll
-      for (int st = 0; st < 2; ++st) T::add(T::col_addr(kb + T::BYTES, lane), 32 * st, s[st], o);
+      for (int st = 0; st < NX; ++st) T::add(T::col_addr(kb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, s[st], o);
     }
     if (it + 1 < n) finish(next, (it + 1) & 1);
     e = next;
     next = list.entry(it + 2 <= list.tiles ? it + 2 : list.tiles);
+  }
+  if (SHARE == 2) {   // the second wave of a group leaves its sums, and the reference that they go by
+    float* room = reinterpret_cast<float*>(smem);
+    float* stat = room + 128 * 16 * T::DT + group * 128;
+    __syncthreads();
+    if (x0) {
+      leave(room, group, lane, o);
+      stat[lane] = m;
+      stat[64 + lane] = lsum;
+    }
+    __syncthreads();
+    if (x0) return;
+    const float m2 = stat[lane], sum2 = stat[64 + lane];
+    const float top = lsum == 0.f ? m2 : sum2 == 0.f ? m : fmaxf(m, m2);
+    const float f = lsum == 0.f ? 0.f : fast_exp2(m - top), f2 = sum2 == 0.f ? 0.f : fast_exp2(m2 - top);
+    take(room, group, lane, o, f, f2);
+    lsum = lsum * f + sum2 * f2;
+    m = top;
   }
   if (!ok) return;
   T::put(static_cast<bf16*>(const_cast<void*>(g.o.p)) + b * g.o.b + (int64_t)i * g.o.t + h * g.o.h, g.dh, half, lsum == 0.f ? 0.f : 1.f / lsum, o);
@@ -408,17 +452,19 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
 // (for dq the correction below comes to exactly 0 by itself, but with a cap)
 constexpr float kOneKey = 1.f - 1.f / 65536.f;
 
-template <int DP, int MOD>
-__global__ __launch_bounds__(256, DP == 64 ? 3 : 1) void rule_dq_kernel(AttnRuleArgs g) {
+template <int DP, int MOD, int SHARE>
+__global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dq_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
+  constexpr int kRows = 128 / SHARE, NX = 2 / SHARE;   // rows of a workgroup; parts of 32 rows of a tile that a wave takes
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   int* kdoc = reinterpret_cast<int*>(smem + 4 * T::BYTES);
-  const RuleList<32> list(kdoc + 2 * kRuleTile, g.Sk);
+  const RuleList<32, SHARE> list(kdoc + 2 * kRuleTile, g.Sk);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  const int nqb = (g.Sq + 127) / 128;
+  const int group = wave / SHARE, x0 = wave % SHARE * NX;   // rows of the wave; its first part of a tile
+  const int nqb = (g.Sq + kRows - 1) / kRows;
   const RuleUnit u(g, nqb, g.H, blockIdx.x, gridDim.x, g.order != 0);
   const int b = u.b, h = u.h, hk = h / (g.H / g.Hkv);
-  const int i = u.blk * 128 + wave * 32 + (lane & 31);
+  const int i = u.blk * kRows + group * 32 + (lane & 31);
   const RuleRows rows(g, b);
   const int lim = rows.lim(g, i), qd = rows.qdoc(g, i);
   const bool ok = i < g.Sq, on = ok && qd >= 0;
@@ -427,7 +473,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 1) void rule_dq_kernel(AttnRule
   T::own(static_cast<const bf16*>(g.d_o.p) + b * g.d_o.b + (int64_t)i * g.d_o.t + h * g.d_o.h, on, g.dh, half, dof);
   const float nlse = on ? -rule_lse2(g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i]) : -INFINITY;
   const float dl = T::own_dot(static_cast<const bf16*>(g.o.p) + b * g.o.b + (int64_t)i * g.o.t + h * g.o.h, on, g.dh, half, dof);
-  const int n = list.build<true>(g, rows, wave, lane, u.blk, qd, ok);
+  const int n = list.template build<true>(g, rows, wave, lane, u.blk, qd, ok);
   const Streams<DP> kv(g.k, hk, g.v, hk, b, wave, lane);
   StreamDocs<DP> sd(rows.k, g.Sk, kv.row);
   const unsigned lds = lds_addr(smem), mine = lds + wave * T::N * 1024;
@@ -457,12 +503,12 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 1) void rule_dq_kernel(AttnRule
       const unsigned kb = lds + (it & 1) * 2 * T::BYTES;
       const int j0 = list.tile(e) * kRuleTile;
       const bool whole = list.whole(e, wave);
-      const float at = (float)(g.q0 + i - j0 - 4 * half);
-      const int far = lim - j0 - 4 * half;
+      const float at = (float)(g.q0 + i - j0 - 32 * x0 - 4 * half);
+      const int far = lim - j0 - 32 * x0 - 4 * half;
 #pragma unroll 1
-      for (int st = 0; st < 2; ++st) {
-        f32x16 s = T::dot(T::row_addr(kb, lane), 32 * st, qf);
-        f32x16 dp = T::dot(T::row_addr(kb + T::BYTES, lane), 32 * st, dof);
+      for (int st = 0; st < NX; ++st) {
+        f32x16 s = T::dot(T::row_addr(kb, lane) + 32 * x0 * T::RB, 32 * st, qf);
+        f32x16 dp = T::dot(T::row_addr(kb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, dof);
         f32x16 w;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
@@ -475,7 +521,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 1) void rule_dq_kernel(AttnRule
 #pragma unroll
           for (int g4 = 0; g4 < 4; ++g4) {
             int kd[4];
-            four(kdoc + (it & 1) * kRuleTile + 32 * st + 8 * g4 + 4 * half, kd);
+            four(kdoc + (it & 1) * kRuleTile + 32 * (x0 + st) + 8 * g4 + 4 * half, kd);
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               const int v = 4 * g4 + x;
@@ -496,7 +542,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 1) void rule_dq_kernel(AttnRule
             w[v] *= f;
           }
         }
-        T::add2(T::col_addr(kb, lane), 32 * st, dp, dq, w, wk, (MOD & 1) ? nullptr : &rounded);
+        T::add2(T::col_addr(kb, lane) + 32 * x0 * T::RB, 32 * st, dp, dq, w, wk, (MOD & 1) ? nullptr : &rounded);
       }
     }
     if (it + 1 < n) finish(next, (it + 1) & 1);
@@ -505,34 +551,54 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 1) void rule_dq_kernel(AttnRule
   }
   rest += half_swap(rest);
   rounded = (MOD & 1) ? rest : rounded + half_swap(rounded);
-  if (!ok) return;
-  if (half == 0) g.delta[((int64_t)b * g.H + h) * g.Sq + i] = on ? dl + rest : 0.f;
+  float* room = reinterpret_cast<float*>(smem);
+  if (SHARE == 2) {   // r is the sum over both waves' keys, and each takes its own part of the product out with it
+    float* stat = room + group * 256;
+    __syncthreads();
+    stat[128 * x0 + lane] = rest;
+    stat[128 * x0 + 64 + lane] = rounded;
+    __syncthreads();
+    const float rest2 = stat[128 * (1 - x0) + lane], rounded2 = stat[128 * (1 - x0) + 64 + lane];
+    rest = x0 ? rest2 + rest : rest + rest2;
+    rounded = x0 ? rounded2 + rounded : rounded + rounded2;
+  }
+  if (SHARE == 1 && !ok) return;
+  if (ok && x0 == 0 && half == 0) g.delta[((int64_t)b * g.H + h) * g.Sq + i] = on ? dl + rest : 0.f;
 #pragma unroll
   for (int dt = 0; dt < T::DT; ++dt)
 #pragma unroll
     for (int v = 0; v < 16; ++v) dq[dt][v] = fmaf(-rounded, wk[dt][v], dq[dt][v]);
+  if (SHARE == 2) {
+    __syncthreads();
+    if (x0) leave(room, group, lane, dq);
+    __syncthreads();
+    if (x0 || !ok) return;
+    take(room, group, lane, dq, 1.f, 1.f);
+  }
   T::put(static_cast<bf16*>(const_cast<void*>(g.dq.p)) + b * g.dq.b + (int64_t)i * g.dq.t + h * g.dq.h, g.dh, half, g.scale, dq);
 }
 
-template <int DP, int MOD>
-__global__ __launch_bounds__(256, DP == 64 ? 3 : 1) void rule_dkv_kernel(AttnRuleArgs g) {
+template <int DP, int MOD, int SHARE>
+__global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dkv_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
+  constexpr int kRows = 128 / SHARE, NX = 2 / SHARE;   // rows of a workgroup; parts of 32 rows of a tile that a wave takes
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   float* stat = reinterpret_cast<float*>(smem + 4 * T::BYTES);                // [2][-lse, delta][64], behind [2][Q tile, dO tile]
   int* info = reinterpret_cast<int*>(stat + 4 * kRuleTile);                   // [2][document, lim][64]
-  const RuleList<32> list(info + 4 * kRuleTile, g.Sq);
+  const RuleList<32, SHARE> list(info + 4 * kRuleTile, g.Sq);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  const int nkb = (g.Sk + 127) / 128, G = g.H / g.Hkv;
+  const int group = wave / SHARE, x0 = wave % SHARE * NX;   // rows of the wave; its first part of a tile
+  const int nkb = (g.Sk + kRows - 1) / kRows, G = g.H / g.Hkv;
   const RuleUnit u(g, nkb, g.Hkv, blockIdx.x, gridDim.x, false);
   const int b = u.b, hk = u.h;
-  const int j = u.blk * 128 + wave * 32 + (lane & 31);
+  const int j = u.blk * kRows + group * 32 + (lane & 31);
   const RuleRows rows(g, b);
   const int kd = rows.kdoc(g, j);
   const bool ok = j < g.Sk, on = ok && kd >= 0;
   bf16x8 kf[T::KS], vf[T::KS];
   T::own(static_cast<const bf16*>(g.k.p) + b * g.k.b + (int64_t)j * g.k.t + hk * g.k.h, on, g.dh, half, kf);
   T::own(static_cast<const bf16*>(g.v.p) + b * g.v.b + (int64_t)j * g.v.t + hk * g.v.h, on, g.dh, half, vf);
-  const int n = list.build<false>(g, rows, wave, lane, u.blk, kd, ok);
+  const int n = list.template build<false>(g, rows, wave, lane, u.blk, kd, ok);
   f32x16 dk[T::DT], dv[T::DT];
 #pragma unroll
   for (int dt = 0; dt < T::DT; ++dt) { dk[dt] = zero16(); dv[dt] = zero16(); }
@@ -584,14 +650,14 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 1) void rule_dkv_kernel(AttnRul
         const float* st2 = stat + (it & 1) * 2 * kRuleTile;
         const int* inf = info + (it & 1) * 2 * kRuleTile;
         const bool whole = list.whole(e, wave);
-        const float at = (float)(g.q0 + list.tile(e) * kRuleTile - j + 4 * half);
+        const float at = (float)(g.q0 + list.tile(e) * kRuleTile + 32 * x0 - j + 4 * half);
 #pragma unroll 1
-        for (int st = 0; st < 2; ++st) {
-          f32x16 s = T::dot(T::row_addr(qb, lane), 32 * st, kf);
-          f32x16 ds = T::dot(T::row_addr(qb + T::BYTES, lane), 32 * st, vf);
+        for (int st = 0; st < NX; ++st) {
+          f32x16 s = T::dot(T::row_addr(qb, lane) + 32 * x0 * T::RB, 32 * st, kf);
+          f32x16 ds = T::dot(T::row_addr(qb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, vf);
 #pragma unroll
           for (int g4 = 0; g4 < 4; ++g4) {
-            const int r0 = 32 * st + 8 * g4 + 4 * half;
+            const int r0 = 32 * (x0 + st) + 8 * g4 + 4 * half;
             const float4 l4 = *reinterpret_cast<const float4*>(st2 + r0);
             const float4 d4 = *reinterpret_cast<const float4*>(st2 + kRuleTile + r0);
             const float nl[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
@@ -620,14 +686,26 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 1) void rule_dkv_kernel(AttnRul
 #pragma unroll
             for (int x = 0; x < 4; ++x) ds[4 * g4 + x] *= s[4 * g4 + x];
           }
-          T::add(T::col_addr(qb + T::BYTES, lane), 32 * st, s, dv);
-          T::add(T::col_addr(qb, lane), 32 * st, ds, dk);
+          T::add(T::col_addr(qb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, s, dv);
+          T::add(T::col_addr(qb, lane) + 32 * x0 * T::RB, 32 * st, ds, dk);
         }
       }
       if (it + 1 < n) finish(next, (it + 1) & 1);
       e = next;
       next = list.entry(it + 2 <= list.tiles ? it + 2 : list.tiles);
     }
+  }
+  if (SHARE == 2) {
+    float* room = reinterpret_cast<float*>(smem);
+    __syncthreads();
+    if (x0) {
+      leave(room, group, lane, dk);
+      leave(room + 128 * 16 * T::DT, group, lane, dv);
+    }
+    __syncthreads();
+    if (x0) return;
+    take(room, group, lane, dk, 1.f, 1.f);
+    take(room + 128 * 16 * T::DT, group, lane, dv, 1.f, 1.f);
   }
   if (ok) {
     T::put(static_cast<bf16*>(const_cast<void*>(g.dk.p)) + b * g.dk.b + (int64_t)j * g.dk.t + hk * g.dk.h, g.dh, half, g.scale, dk);
@@ -646,14 +724,23 @@ hipError_t launch(K kernel, int blocks, size_t lds, const AttnRuleArgs& g, hipSt
   hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), lds, st, g);
   return hipGetLastError();
 }
+// Blocks of 128 rows, or of 64 with two waves for 32 rows where there would be fewer of those than CUs.
+constexpr int kCUs = 256;
+int blocks_of(int groups, int rows, int each) { return groups * ((rows + each - 1) / each); }
+
 template <int DP, int MOD>
 hipError_t launch_fwd(const AttnRuleArgs& g, hipStream_t st) {
-  return launch(rule_fwd_kernel<DP, MOD>, g.nb * g.H * ((g.Sq + 127) / 128), lds_bytes<DP>(g.Sk, false), g, st);
+  const int heads = g.nb * g.H, whole = blocks_of(heads, g.Sq, 128);
+  const size_t lds = lds_bytes<DP>(g.Sk, false);
+  return whole < kCUs ? launch(rule_fwd_kernel<DP, MOD, 2>, blocks_of(heads, g.Sq, 64), lds, g, st) : launch(rule_fwd_kernel<DP, MOD, 1>, whole, lds, g, st);
 }
 template <int DP, int MOD>
 hipError_t launch_bwd(const AttnRuleArgs& g, hipStream_t st) {
-  const hipError_t e = launch(rule_dq_kernel<DP, MOD>, g.nb * g.H * ((g.Sq + 127) / 128), lds_bytes<DP>(g.Sk, false), g, st);
-  return e != hipSuccess ? e : launch(rule_dkv_kernel<DP, MOD>, g.nb * g.Hkv * ((g.Sk + 127) / 128), lds_bytes<DP>(g.Sq, true), g, st);
+  const int heads = g.nb * g.H, key_heads = g.nb * g.Hkv, whole_q = blocks_of(heads, g.Sq, 128), whole_k = blocks_of(key_heads, g.Sk, 128);
+  const size_t lds_q = lds_bytes<DP>(g.Sk, false), lds_k = lds_bytes<DP>(g.Sq, true);
+  const hipError_t e = whole_q < kCUs ? launch(rule_dq_kernel<DP, MOD, 2>, blocks_of(heads, g.Sq, 64), lds_q, g, st) : launch(rule_dq_kernel<DP, MOD, 1>, whole_q, lds_q, g, st);
+  if (e != hipSuccess) return e;
+  return whole_k < kCUs ? launch(rule_dkv_kernel<DP, MOD, 2>, blocks_of(key_heads, g.Sk, 64), lds_k, g, st) : launch(rule_dkv_kernel<DP, MOD, 1>, whole_k, lds_k, g, st);
 }
 template <int DP>
 hipError_t by_mod(const AttnRuleArgs& g, bool bwd, hipStream_t st) {
