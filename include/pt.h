@@ -348,8 +348,9 @@ PT_API pt_status pt_profile_read(pt_ctx* ctx, int32_t category, double* total_ms
  * both are of the same document: documents are ids >= 0 in any order; a
  * negative id marks padding, which sees nothing and which nothing sees.  The
  * rows of q, k, v and d_o that belong to padding are never used, whatever they
- * hold (NaN too); a NaN or an infinity elsewhere may also reach queries of other
- * documents in the same rows of 64.  A query that sees no key has o = 0,
+ * hold (NaN too); a NaN or an infinity in another row may also reach rows that
+ * it is hidden from (by the order or its document), as it would through products
+ * with probabilities of 0.  A query that sees no key has o = 0,
  * lse = -infinity and no gradient; so have padding rows, which are written as
  * zeros.  Head h reads key and value head h / (H / Hkv), whose gradients are
  * the sums over the heads that share it.  Slopes, documents and prefix lengths

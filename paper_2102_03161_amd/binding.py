@@ -250,6 +250,8 @@ def _heads(t, name: str, shape, dtype) -> tuple:
 
 
 def _plain(t, dtype, shape, name: str):
+    if t is None:
+        _refuse(f"{name} is None")
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         _refuse(f"{name}: {dtype} {list(shape)}, contiguous (got {t.dtype} {list(t.shape)})")
     return t.data_ptr()
@@ -270,7 +272,7 @@ class AttentionRule:
     def __init__(self, order="full", scale=None, cap=0.0, slopes=None, documents=None, q_documents=None, prefix=None, q0=0):
         if order not in ATTN_ORDERS:
             _refuse(f"order {order!r}: one of {', '.join(ATTN_ORDERS)}")
-        if not 0 <= q0 < 1 << 24 or not 0.0 <= cap <= 3e38 or not (scale is None or 0.0 < scale <= 3e38):
+        if not 0 <= q0 < 1 << 24 or not (cap == 0.0 or 1e-38 <= cap <= 3e38) or not (scale is None or 0.0 < scale <= 3e38):
             _refuse(f"q0 {q0}, cap {cap}, scale {scale}: q0 in 0 .. 2^24, cap not negative, scale positive")
         self.order, self.scale, self.cap, self.q0 = order, scale, cap, q0
         self.slopes, self.documents, self.prefix = slopes, documents, prefix

@@ -6,8 +6,8 @@
 //
 // What a query sees: keys up to lim_i (its own position, the end of the sample's prefix, or the last key) of its own document.
 //
-// One wave owns 32 rows (queries in the forward pass and for dq, keys for dk / dv); a workgroup of four waves streams the other
-// side through LDS in tiles of 64 rows.  Scores are computed with the owned row as the MFMA's column, so that softmax statistics
+// One wave owns 32 rows (queries in the forward pass and for dq, keys for dk / dv), or, where that makes too few workgroups, half of
+// the streamed rows of 32 rows, joined at the end; a workgroup of four waves streams the other side through LDS in tiles of 64 rows.  Scores are computed with the owned row as the MFMA's column, so that softmax statistics
 // are one value per lane and the probabilities, rounded to bf16, are the next MFMA's operand as they stand in registers.
 //
 // Work that a mask leaves out is not done: before anything else a workgroup writes the list of the tiles that any of its waves
@@ -449,7 +449,9 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
 // the r of that product is summed from dS as it was rounded to bf16 for the other (two to an instruction): the part of those
 // roundings that all keys share, which dS itself, summing to 0, does not have, then cancels.
 // p of 1 means a query that sees one key: dS is exactly 0 then, where dP - delta would leave the rounding of two different sums
-// (for dq the correction below comes to exactly 0 by itself, but with a cap)
+// (for dq the correction below comes to exactly 0 by itself, but with a cap).  The rounding of lse leaves p short of 1 by 2^-23 |lse|
+// log2(e), hence the margin; where more keys are visible and one has all but 2^-16 of the weight, the |dS| <= 2^-16 (max dP - min dP)
+// that is left out is a 128th of the rounding of dP's own operands.
 constexpr float kOneKey = 1.f - 1.f / 65536.f;
 
 template <int DP, int MOD, int SHARE>
@@ -724,23 +726,37 @@ hipError_t launch(K kernel, int blocks, size_t lds, const AttnRuleArgs& g, hipSt
   hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), lds, st, g);
   return hipGetLastError();
 }
-// Blocks of 128 rows, or of 64 with two waves for 32 rows where there would be fewer of those than CUs.
-constexpr int kCUs = 256;
+// Blocks of 128 rows, or blocks of 64 with two waves for 32 rows where those of 128 would leave CUs without one.  Measured, blocks of
+// 64 against 128, forward / backward: 1 x 384 rows x 8 heads of 64 9.9 / 24 us against 11.5 / 34; 3 x 1692 x 4, ordered, 31 / 77
+// against 35 / 110; 8 x 663 x 2 heads of 128 20 / 59 against 26 / 81.  With a block for every CU the joins cost more than they give:
+// 12 x 384 x 10 15 / 55 against 16 / 49, 2 x 2048 x 12 heads of 128 in documents 41 / 160 against 33 / 140.  Ordered rows without
+// documents differ in length by their place, and up to two blocks a CU the smaller blocks even that out: 3 x 2048 x 8 49 / 120 against
+// 52 / 162, 1 x 4096 x 16 80 / 211 against 93 / 299.  Heads of 128 gain from it in the forward pass of long rows alone: 1 x 4096 x 16
+// 124 / 575 against 148 / 451, 4 x 1024 x 12 47 / 187 against 45 / 178.
+constexpr int kCUs = 256, kLongRow = 2048;
 int blocks_of(int groups, int rows, int each) { return groups * ((rows + each - 1) / each); }
+template <int DP>
+bool two_waves(const AttnRuleArgs& g, int whole, bool bwd) {
+  const bool uneven = g.order && !g.qdoc && (DP == 64 || (!bwd && g.Sk >= kLongRow));
+  return uneven ? whole <= 2 * kCUs : whole < kCUs;
+}
 
 template <int DP, int MOD>
 hipError_t launch_fwd(const AttnRuleArgs& g, hipStream_t st) {
   const int heads = g.nb * g.H, whole = blocks_of(heads, g.Sq, 128);
   const size_t lds = lds_bytes<DP>(g.Sk, false);
-  return whole < kCUs ? launch(rule_fwd_kernel<DP, MOD, 2>, blocks_of(heads, g.Sq, 64), lds, g, st) : launch(rule_fwd_kernel<DP, MOD, 1>, whole, lds, g, st);
+  return two_waves<DP>(g, whole, false) ? launch(rule_fwd_kernel<DP, MOD, 2>, blocks_of(heads, g.Sq, 64), lds, g, st)
+                                        : launch(rule_fwd_kernel<DP, MOD, 1>, whole, lds, g, st);
 }
 template <int DP, int MOD>
 hipError_t launch_bwd(const AttnRuleArgs& g, hipStream_t st) {
   const int heads = g.nb * g.H, key_heads = g.nb * g.Hkv, whole_q = blocks_of(heads, g.Sq, 128), whole_k = blocks_of(key_heads, g.Sk, 128);
   const size_t lds_q = lds_bytes<DP>(g.Sk, false), lds_k = lds_bytes<DP>(g.Sq, true);
-  const hipError_t e = whole_q < kCUs ? launch(rule_dq_kernel<DP, MOD, 2>, blocks_of(heads, g.Sq, 64), lds_q, g, st) : launch(rule_dq_kernel<DP, MOD, 1>, whole_q, lds_q, g, st);
+  const hipError_t e = two_waves<DP>(g, whole_q, true) ? launch(rule_dq_kernel<DP, MOD, 2>, blocks_of(heads, g.Sq, 64), lds_q, g, st)
+                                                       : launch(rule_dq_kernel<DP, MOD, 1>, whole_q, lds_q, g, st);
   if (e != hipSuccess) return e;
-  return whole_k < kCUs ? launch(rule_dkv_kernel<DP, MOD, 2>, blocks_of(key_heads, g.Sk, 64), lds_k, g, st) : launch(rule_dkv_kernel<DP, MOD, 1>, whole_k, lds_k, g, st);
+  return two_waves<DP>(g, whole_k, true) ? launch(rule_dkv_kernel<DP, MOD, 2>, blocks_of(key_heads, g.Sk, 64), lds_k, g, st)
+                                         : launch(rule_dkv_kernel<DP, MOD, 1>, whole_k, lds_k, g, st);
 }
 template <int DP>
 hipError_t by_mod(const AttnRuleArgs& g, bool bwd, hipStream_t st) {

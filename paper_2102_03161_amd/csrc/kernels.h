@@ -77,6 +77,7 @@ struct AttnRuleArgs {
   float* delta;              // backward in bf16: scratch [nb, H, Sq]
 };
 constexpr int kRuleMaxRows = 1 << 18;   // of queries or keys: the list of tiles lives in LDS
+constexpr int64_t kRuleMaxBlocks = 1 << 23;   // blocks of 64 rows, queries' and keys' together: a launch has fewer than 2^31 threads
 hipError_t attention_rule_fwd(int dt, const AttnRuleArgs& g, hipStream_t st);
 hipError_t attention_rule_bwd(int dt, const AttnRuleArgs& g, hipStream_t st);
 hipError_t attention_rule_bf16(const AttnRuleArgs& g, bool bwd, hipStream_t st);

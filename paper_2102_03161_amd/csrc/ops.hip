@@ -55,9 +55,9 @@ pt_status check_attention(const pt_attention* a) {
     return fail(PT_EINVAL, "documents of the queries and of the keys go together");
   if (!(a->scale > 0.f) || !std::isfinite(a->scale * 3.f)) return fail(PT_EINVAL, "scale must be positive and finite");
   if (!(a->cap >= 0.f) || !std::isfinite(a->cap * 3.f) || (a->cap > 0.f && !std::isfinite(a->scale * 3.f / a->cap))) return fail(PT_EINVAL, "cap must be 0 or a positive finite number");
-  // one launch covers the owned blocks of 64 rows of both passes
-  const int64_t blocks = (int64_t)a->nb * a->H * ((a->Sq + 63) / 64) + (int64_t)a->nb * a->Hkv * ((a->Sk + 63) / 64);
-  if (blocks >= (1 << 24)) return fail(PT_EINVAL, "nb * H * Sq or nb * Hkv * Sk too large");
+  const int64_t heads = (int64_t)a->nb * a->H;
+  if (heads >= kRuleMaxBlocks || heads * ((a->Sq + 63) / 64) + (int64_t)a->nb * a->Hkv * ((a->Sk + 63) / 64) >= kRuleMaxBlocks)
+    return fail(PT_EINVAL, "nb * H * Sq or nb * Hkv * Sk too large");
   return PT_OK;
 }
 AttnRuleArgs rule_args(const pt_attention* a) {
@@ -120,8 +120,8 @@ pt_status pt_attention_bwd(const pt_attention* a, const pt_heads* q, const pt_he
   if (s == PT_OK) s = check_view("dv", dv, a->nb, a->Sk, a->Hkv, a->dtype, true);
   if (s != PT_OK) return s;
   if (a->nb == 0) return PT_OK;
+  if (!lse && a->Sq > 0) return fail(PT_EINVAL, "lse is NULL");
   if (need > 0) {
-    if (!lse) return fail(PT_EINVAL, "lse is NULL");
     if (!ws || ws_bytes < need) return fail(PT_ENOMEM, "the workspace needs %zu bytes", need);
     if (!aligned16(ws)) return fail(PT_EINVAL, "the workspace must be 16-byte aligned");
   }

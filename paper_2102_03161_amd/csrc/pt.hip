@@ -1082,7 +1082,7 @@ pt_status pt_set_attention(pt_ctx* c, const pt_attention_rule* r) {
   if (!(r->cap >= 0.f) || !std::isfinite(r->cap * 3.f) || (r->cap > 0.f && !std::isfinite(3.f / r->cap))) return fail(c, PT_EINVAL, "cap must be 0 or a positive finite number");
   if (r->order == PT_ATTN_PREFIX && !r->prefix) return fail(c, PT_EINVAL, "PT_ATTN_PREFIX needs prefix lengths");
   if ((r->documents || r->prefix) && (r->n < 1 || r->n > g.B)) return fail(c, PT_EINVAL, "n outside 1..B");
-  if (g.S > kRuleMaxRows || 2 * (int64_t)g.B * g.H * ((g.S + 63) / 64) >= (1 << 24)) return fail(c, PT_EINVAL, "batch or sequence too long for attention under a rule");
+  if (g.S > kRuleMaxRows || 2 * (int64_t)g.B * g.H * ((g.S + 63) / 64) >= kRuleMaxBlocks) return fail(c, PT_EINVAL, "batch or sequence too long for attention under a rule");
   if (r->documents) HIP_TRY(c, hipMemcpyAsync(c->w(p.DOCS), r->documents, (size_t)r->n * g.S * 4, hipMemcpyDeviceToDevice, c->st));
   if (r->order == PT_ATTN_PREFIX) HIP_TRY(c, hipMemcpyAsync(c->w(p.PREFIX), r->prefix, (size_t)r->n * 4, hipMemcpyDeviceToDevice, c->st));
   if (r->slopes) HIP_TRY(c, hipMemcpyAsync(c->w(p.SLOPES), r->slopes, (size_t)g.H * 4, hipMemcpyDeviceToDevice, c->st));

@@ -66,6 +66,28 @@ def test_backward_needs_its_statistics_and_workspace():
     assert call(FAR, FAR, need.value, dk=view(head=0)) == binding.PT_EINVAL
 
 
+def test_backward_needs_its_statistics_in_fp32_too():
+    """fp32 takes no workspace, but reads lse all the same."""
+    lib, a = binding.load_library(), description(dtype=binding.PT_F32)
+    args = [view()] * 4 + [None] + [view()] * 4
+    assert lib.pt_attention_bwd(a, *args, None, 0, None) == binding.PT_EINVAL and b"lse" in lib.pt_last_error(None)
+
+
+@pytest.mark.parametrize("over", [dict(nb=1 << 30, H=1 << 30, Hkv=1 << 30, Sq=1 << 18), dict(nb=1 << 16, H=1 << 16, Hkv=1, Sq=0), dict(nb=1 << 24, H=1, Hkv=1, Sq=0, Sk=0)],
+                         ids=["product past 64 bits", "no queries", "nothing but samples"])
+def test_counts_of_heads_that_pass_32_bits(over):
+    assert forward(description(**over))[0] == binding.PT_EINVAL
+
+
+def test_a_cap_that_float_rounds_to_none():
+    for cap in (1e-50, -1.0, float("nan")):
+        with pytest.raises(binding.PtError):
+            binding.AttentionRule(cap=cap)
+    with pytest.raises(binding.PtError, match="lse"):
+        q = torch.zeros(2, 10, 4, 64, dtype=torch.bfloat16)
+        binding.attention_backward(q, q, q, q, None, q)
+
+
 def test_gelu8():
     lib = binding.load_library()
     f = lambda dtype=1, h=FAR, g=FAR, codes=FAR, exps=FAR, rows=4, F=64: lib.pt_gelu8_fwd(dtype, h, g, codes, exps, rows, F, None)   # noqa: E731
