@@ -295,6 +295,20 @@ __device__ __forceinline__ void take(const float* room, int group, int lane, f32
   }
 }
 
+// Weights are rounded to bf16 for the second products, which adds as much error again as the results' own rounding (1.4 times in
+// all), on average over many weights.  Where a sample and head has few pairs, and there are few of those, nothing averages, and what
+// the rounding left out goes through one more product: 3 x 64 rows x 4 heads then take 5.8 / 14.7 us forward / backward, 5.7 / 13.9
+// without; the branch alone costs the longer rows of these grids 1 % forward and up to 4 % backward.
+constexpr int64_t kFewPairs = 4096;
+template <int SHARE>
+__device__ __forceinline__ bool few_pairs(const AttnRuleArgs& g) { return SHARE == 2 && (int64_t)g.Sq * g.Sk <= kFewPairs; }
+__device__ __forceinline__ f32x16 left_out(const f32x16& w) {
+  f32x16 r;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) r[v] = w[v] - to_f32(from_f32<bf16>(w[v]));
+  return r;
+}
+
 // A row's reference m (log2 domain) only has to keep exp2 in range: it is the maximum of the first tile in which the row sees
 // anything, and moves only when a tile's sum passes 2^40.  So a tile whose rows all have one needs no maximum at all.
 constexpr float kGrown = 1099511627776.f;   // 2^40
@@ -410,7 +424,10 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
       }
       lsum += sum + half_swap(sum);
 #pragma unroll
-      for (int st = 0; st < NX; ++st) T::add(T::col_addr(kb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, s[st], o);
+      for (int st = 0; st < NX; ++st) {
+        T::add(T::col_addr(kb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, s[st], o);
+        if (few_pairs<SHARE>(g)) T::add(T::col_addr(kb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, left_out(s[st]), o);
+      }
     }
     if (it + 1 < n) finish(next, (it + 1) & 1);
     e = next;
@@ -449,7 +466,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
 // the r of that product is summed from dS as it was rounded to bf16 for the other (two to an instruction): the part of those
 // roundings that all keys share, which dS itself, summing to 0, does not have, then cancels.
 // p of 1 means a query that sees one key: dS is exactly 0 then, where dP - delta would leave the rounding of two different sums
-// (for dq the correction below comes to exactly 0 by itself, but with a cap).  The rounding of lse leaves p short of 1 by 2^-23 |lse|
+// (for dq the correction below comes to exactly 0 by itself where the weight is rounded to 1 and there is no cap).  The rounding of lse leaves p short of 1 by 2^-23 |lse|
 // log2(e), hence the margin; where more keys are visible and one has all but 2^-16 of the weight, the |dS| <= 2^-16 (max dP - min dP)
 // that is left out is a 128th of the rounding of dP's own operands.
 constexpr float kOneKey = 1.f - 1.f / 65536.f;
@@ -484,6 +501,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dq_kernel(
 #pragma unroll
   for (int dt = 0; dt < T::DT; ++dt) { dq[dt] = zero16(); wk[dt] = zero16(); }
   float rest = 0.f, rounded = 0.f;   // r, and r from dS as it was rounded
+  const bool few = few_pairs<SHARE>(g);
   auto load = [&](int e, int at) {
     const int j0 = list.tile(e) * kRuleTile;
     sd.load(j0);
@@ -527,8 +545,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dq_kernel(
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               const int v = 4 * g4 + x;
-              // with a cap the correction below is no exact 0 for a query that sees one key
-              if ((MOD & 1) && w[v] >= kOneKey) dp[v] = 0.f;
+              // the correction below is an exact 0 for a query that sees one key only where its weight is rounded to 1
+              if (((MOD & 1) || few) && w[v] >= kOneKey) dp[v] = 0.f;
               w[v] = kd[x] == qd ? w[v] : 0.f;
               if (g.order != 0) w[v] = 32 * st + 8 * g4 + x <= far ? w[v] : 0.f;
             }
@@ -545,6 +563,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dq_kernel(
           }
         }
         T::add2(T::col_addr(kb, lane) + 32 * x0 * T::RB, 32 * st, dp, dq, w, wk, (MOD & 1) ? nullptr : &rounded);
+        if (few)
+          T::add2(T::col_addr(kb, lane) + 32 * x0 * T::RB, 32 * st, left_out(dp), dq, left_out(w), wk, (MOD & 1) ? nullptr : &rounded);
       }
     }
     if (it + 1 < n) finish(next, (it + 1) & 1);
@@ -690,6 +710,10 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dkv_kernel
           }
           T::add(T::col_addr(qb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, s, dv);
           T::add(T::col_addr(qb, lane) + 32 * x0 * T::RB, 32 * st, ds, dk);
+          if (few_pairs<SHARE>(g)) {
+            T::add(T::col_addr(qb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, left_out(s), dv);
+            T::add(T::col_addr(qb, lane) + 32 * x0 * T::RB, 32 * st, left_out(ds), dk);
+          }
         }
       }
       if (it + 1 < n) finish(next, (it + 1) & 1);

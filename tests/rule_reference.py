@@ -8,8 +8,10 @@ import torch
 E32 = 2.0 ** -24
 
 
-def reference(q, k, v, do=None, order="full", scale=None, cap=0.0, slopes=None, q_docs=None, k_docs=None, prefix=None, q0=0):
-    """q [nb, Sq, H, dh] etc. of any type; returns {name: (value, bound)} in float64 for o, lse and, with do, dq, dk, dv."""
+def reference(q, k, v, do=None, order="full", scale=None, cap=0.0, slopes=None, q_docs=None, k_docs=None, prefix=None, q0=0, few=False):
+    """q [nb, Sq, H, dh] etc. of any type; returns {name: (value, bound)} in float64 for o, lse and, with do, dq, dk, dv.  few: the
+    bound of calls of few pairs, where what a weight's rounding leaves out is rounded by itself (u u of the weight is lost) and delta
+    does not go by the rounded o."""
     bf16 = q.dtype == torch.bfloat16
     u = 2.0 ** -8 if bf16 else E32
     nb, Sq, H, dh = q.shape
@@ -53,8 +55,9 @@ def reference(q, k, v, do=None, order="full", scale=None, cap=0.0, slopes=None, 
     dp_rel = 2.1 * off + (Sk + 16) * E32 + 8 * E32 * fin.abs()          # relative error of a probability
     o = p @ V
     aV = p @ V.abs()
-    up = u if bf16 else 0.0
-    o_err = (up + dp_rel + (Sk + 2) * E32) * aV * (1 + u) + u * o.abs()
+    up = (u * u if few else u) if bf16 else 0.0
+    sum_err = (up + dp_rel + (Sk + 2) * E32) * aV * (1 + u)
+    o_err = sum_err + u * o.abs()
     back = lambda x: x.permute(0, 2, 1, 3)   # noqa: E731
     out = {"o": (back(o), back(o_err)),
            "lse": (lse[..., 0], (off + (Sk + 16) * E32 + 8 * E32 * fin.abs())[..., 0])}
@@ -63,7 +66,7 @@ def reference(q, k, v, do=None, order="full", scale=None, cap=0.0, slopes=None, 
     dO = wide(do, live_q)
     dP = dO @ V.transpose(2, 3)
     delta = (p * dP).sum(-1, keepdim=True)
-    delta_err = (dO.abs() * o_err).sum(-1, keepdim=True) + dh * E32 * (dO.abs() * o.abs()).sum(-1, keepdim=True)
+    delta_err = (dO.abs() * (sum_err + u ** 3 * o.abs() if few else o_err)).sum(-1, keepdim=True) + dh * E32 * (dO.abs() * o.abs()).sum(-1, keepdim=True)
     dP_err = (dh + 2) * E32 * (dO.abs() @ V.abs().transpose(2, 3))
     slope = 1.0 - bent * bent
     dS = p * (dP - delta) * slope

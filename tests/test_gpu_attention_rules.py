@@ -243,3 +243,13 @@ def test_lengths_of_zero():
         for name in ("o", "dq", "dk", "dv"):
             assert not got[name].any(), (name, nb, Sq, Sk)
         assert (got["lse"] == -float("inf")).all()
+
+
+@pytest.mark.parametrize("cap,order,S", [(0.0, "full", 64), (20.0, "causal", 64), (0.0, "prefix", 33), (0.0, "full", 3)])
+def test_few_pairs_keep_what_rounding_their_weights_leaves_out(cap, order, S):
+    gen = torch.Generator().manual_seed(77)
+    q, k, v, do = inputs(2, S, S, 4, 2, 64, BF16, gen)
+    rule = dict(order=order, cap=cap, prefix=torch.tensor([5, 20], dtype=torch.int32) if order == "prefix" else None)
+    want, got = reference(q, k, v, do, few=True, **rule), both(q, k, v, do, **rule)
+    for name in want:
+        check(name, got[name], want[name])
