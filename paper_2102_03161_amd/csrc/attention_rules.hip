@@ -13,6 +13,14 @@
 // Work that a mask leaves out is not done: before anything else a workgroup writes the list of the tiles that any of its waves
 // needs, each with four bits "this wave needs it" and four bits "all 32 x 64 pairs of this wave are visible".  Only tiles without
 // the latter bit are masked pair by pair.  The list is built from the documents' ids as they are, in any order.
+//
+// What bounds it: per pair and head the forward pass takes 4 dh flops of MFMA and about 2.5 VALU instructions (exp2 is a quarter
+// rate one), dq 8 dh (two products for the score and dP, two for dq and its correction), dk / dv 8 dh; at a head size of 64 the
+// VALU work takes about as long as the MFMAs, and of the four waves of a SIMD only some overlap the two: 740 - 830 TFLOP/s forward in
+// the steady state, 840 - 920 at 128 (a large product reaches 1444).  Measured: 32 x 384 rows x 12 heads of 64, padded, 39 us
+// forward, 59 dq, 61 dk / dv; 4 x 2048 x 16 packed, prefix, cap 68 / 113 / 119; 1 x 8192 x 16 of 128, causal, 4 key heads, forward
+// 322 (855 TFLOP/s of the visible pairs).  Tiles of 64 rows: two buffers of two take 32 KB at a head size of 64, so four workgroups
+// fit a CU and hide each other's barriers, first loads and lists.
 #include <algorithm>
 
 #include "attention_rules.h"
@@ -269,7 +277,8 @@ __device__ __forceinline__ void four(const int* p, int (&x)[4]) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
-// forward
+// forward: one pass over the tiles with the running reference and sum of a softmax; four workgroups a CU at a head size of 64 (126
+// registers), two at 128.  At short rows it is bound by starting up: of 39 us for 32 x 384 x 12 the products take 18.
 // ---------------------------------------------------------------------------------------------------------------------------
 // Two waves that share their rows: the second one's accumulators through LDS (both buffers' tiles, which nothing reads any more),
 // 16 bytes a lane next to each other.
@@ -457,7 +466,10 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
-// backward: dq (128 queries a workgroup), which also leaves each query's delta, then dk and dv (128 keys a workgroup)
+// backward: dq (128 queries a workgroup), which also leaves each query's delta, then dk and dv (128 keys a workgroup, the heads that
+// share them one after the other).  Two launches, because no workgroup sees all of a row and a column, and sums by atomics would
+// depend on their order.  Three workgroups a CU at a head size of 64 (168 registers); 272 - 312 registers at 128, one wave a SIMD,
+// which then waits for its own LDS reads: 12 x 384 rows x 10 heads of 128 take 108 us, of 64 49.
 // ---------------------------------------------------------------------------------------------------------------------------
 // delta_i = dO_i . o_i with o rounded to bf16 is off by 2^-9 of |dO||o|, which for a query with few keys, or one that takes most
 // of the weight, is as large as dS itself.  So the pass uses that value d only to centre dP, and takes out what is left of it:

@@ -9,7 +9,10 @@
 //   backward  dh = dg (Phi(x) + x phi(x)), and g = x Phi(x) again for the weight gradient that reads it
 //
 // Both are one pass; a thread holds 16 bytes of a row (8 bytes where rows of bf16 are an odd multiple of 4 values long), a block
-// of 32 is 4 or 8 neighbouring lanes.
+// of 32 is 4 or 8 neighbouring lanes.  Memory bounds both: in bf16 a value moves 5 bytes forward (2 in, 2 + 1 out) and 7 back.
+// 32768 x 4096 values take 114 us forward (5.9 TB/s) and 160 back (5.9 TB/s), where a large copy reaches 5.1 TB/s (its reads and
+// writes are equal, these read more or less than they write); 12608 x 1540, in pieces of 8 bytes, 25 us back (5.5 TB/s); 231 x 1024
+// 3 us each, a launch.
 #include "common.h"
 #include "kernels.h"
 
