@@ -763,18 +763,20 @@ hipError_t launch(K kernel, int blocks, size_t lds, const AttnRuleArgs& g, hipSt
   return hipGetLastError();
 }
 // Blocks of 128 rows, or blocks of 64 with two waves for 32 rows where those of 128 would leave CUs without one.  Measured, blocks of
-// 64 against 128, forward / backward: 1 x 384 rows x 8 heads of 64 9.9 / 24 us against 11.5 / 34; 3 x 1692 x 4, ordered, 31 / 77
-// against 35 / 110; 8 x 663 x 2 heads of 128 20 / 59 against 26 / 81.  With a block for every CU the joins cost more than they give:
-// 12 x 384 x 10 15 / 55 against 16 / 49, 2 x 2048 x 12 heads of 128 in documents 41 / 160 against 33 / 140.  Ordered rows without
-// documents differ in length by their place, and up to two blocks a CU the smaller blocks even that out: 3 x 2048 x 8 49 / 120 against
-// 52 / 162, 1 x 4096 x 16 80 / 211 against 93 / 299.  Heads of 128 gain from it in the forward pass of long rows alone: 1 x 4096 x 16
-// 124 / 575 against 148 / 451, 4 x 1024 x 12 47 / 187 against 45 / 178.
-constexpr int kCUs = 256, kLongRow = 2048;
+// 64 against 128, forward / backward: 1 x 384 rows x 8 heads of 64 9.9 / 24 us against 11.5 / 34; 8 x 663 x 2 heads of 128 20 / 59
+// against 26 / 81.  Ordered rows without documents differ in length by their place, and up to two blocks a CU the smaller blocks even
+// that out: 3 x 2048 x 8 38 / 107 against 45 / 143, 1 x 4096 x 16 69 / 214 against 78 / 264.  So they do for every rule in the forward pass at
+// a head size of 64, whose registers leave room for them (12 x 384 x 10 15 against 16, 2 x 2048 x 12 in documents 22 against 24), but
+// not back: 55 against 49, 72 against 66.  Heads of 128 take them forward for ordered rows (1 x 3441 x 12 81 against 112, but 2 x 2048
+// x 12 in documents 38 against 33); backward only up to one block a CU, where the longest is all that counts (1 x 8192 x 16 on 4 key
+// heads 1760 against 2360, but 1 x 4096 x 16 555 against 430).
+constexpr int kCUs = 256;
 int blocks_of(int groups, int rows, int each) { return groups * ((rows + each - 1) / each); }
 template <int DP>
 bool two_waves(const AttnRuleArgs& g, int whole, bool bwd) {
-  const bool uneven = g.order && !g.qdoc && (DP == 64 || (!bwd && g.Sk >= kLongRow));
-  return uneven ? whole <= 2 * kCUs : whole < kCUs;
+  const bool uneven = g.order && !g.qdoc;
+  const bool twice = bwd ? uneven && DP == 64 : uneven || DP == 64;
+  return twice ? whole <= 2 * kCUs : uneven ? whole <= kCUs : whole < kCUs;
 }
 
 template <int DP, int MOD>
