@@ -88,12 +88,12 @@ __device__ __forceinline__ int rule_wave_min(int v) {
 }
 __device__ __forceinline__ int rule_wave_max(int v) { return ~rule_wave_min(~v); }
 
-// The tiles that a workgroup of four waves visits, SHARE waves owning ROWS rows together: entries tile << 9 | plain << 8 | whole bits << 4 |
-// needed bits.  plain: all its rows exist and none is padding.
+// The tiles that a workgroup of four waves visits, SHARE waves owning ROWS rows together: entries tile << 9 | plain << 8 |
+// whole bits << 4 | needed bits.  plain: all its rows exist and none is padding.
 // In LDS: the least and the largest document of each wave's rows and of each tile (the sign of the least says that padding is among
-// them, that of the largest that padding or several documents are), then, in place of the tiles' least, the entries.  A tile is needed by a wave whose range of
-// documents meets its own and whose positions reach it; it is whole if both are one and the same document and all positions of
-// the wave see all of the tile.
+// them, that of the largest that padding or several documents are), then, in place of the tiles' least, the entries.  A tile is
+// needed by a wave whose range of documents meets its own and whose positions reach it; it is whole if both are one and the same
+// document and all positions of the wave see all of the tile.
 template <int ROWS, int SHARE = 1>
 struct RuleList {
   int* base;

@@ -7,8 +7,9 @@
 // What a query sees: keys up to lim_i (its own position, the end of the sample's prefix, or the last key) of its own document.
 //
 // One wave owns 32 rows (queries in the forward pass and for dq, keys for dk / dv), or, where that makes too few workgroups, half of
-// the streamed rows of 32 rows, joined at the end; a workgroup of four waves streams the other side through LDS in tiles of 64 rows.  Scores are computed with the owned row as the MFMA's column, so that softmax statistics
-// are one value per lane and the probabilities, rounded to bf16, are the next MFMA's operand as they stand in registers.
+// the streamed rows of 32 rows, joined at the end; a workgroup of four waves streams the other side through LDS in tiles of 64 rows.
+// Scores are computed with the owned row as the MFMA's column, so that softmax statistics are one value per lane and the
+// probabilities, rounded to bf16, are the next MFMA's operand as they stand in registers.
 //
 // Work that a mask leaves out is not done: before anything else a workgroup writes the list of the tiles that any of its waves
 // needs, each with four bits "this wave needs it" and four bits "all 32 x 64 pairs of this wave are visible".  Only tiles without
@@ -18,8 +19,8 @@
 // rate one), dq 8 dh (two products for the score and dP, two for dq and its correction), dk / dv 8 dh; at a head size of 64 the
 // VALU work takes about as long as the MFMAs, and of the four waves of a SIMD only some overlap the two: 740 - 830 TFLOP/s forward in
 // the steady state, 840 - 920 at 128 (a large product reaches 1444).  Measured: 32 x 384 rows x 12 heads of 64, padded, 39 us
-// forward, 59 dq, 61 dk / dv; 4 x 2048 x 16 packed, prefix, cap 68 / 113 / 119; 1 x 8192 x 16 of 128, causal, 4 key heads, forward
-// 322 (855 TFLOP/s of the visible pairs).  Tiles of 64 rows: two buffers of two take 32 KB at a head size of 64, so four workgroups
+// forward, 59 dq, 61 dk / dv; 4 x 2048 x 16 packed, prefix, cap 61 / 107 / 89; 1 x 8192 x 16 of 128, causal, 4 key heads, forward
+// 317 (867 TFLOP/s of the visible pairs).  Tiles of 64 rows: two buffers of two take 32 KB at a head size of 64, so four workgroups
 // fit a CU and hide each other's barriers, first loads and lists.
 #include <algorithm>
 
@@ -278,7 +279,7 @@ __device__ __forceinline__ void four(const int* p, int (&x)[4]) {
 
 // ---------------------------------------------------------------------------------------------------------------------------
 // forward: one pass over the tiles with the running reference and sum of a softmax; four workgroups a CU at a head size of 64 (126
-// registers), two at 128.  At short rows it is bound by starting up: of 39 us for 32 x 384 x 12 the products take 18.
+// registers), two at 128.  At short rows it is bound by starting up: of 39 us for 32 x 384 x 12, padded, the visible pairs' products take 5.
 // ---------------------------------------------------------------------------------------------------------------------------
 // Two waves that share their rows: the second one's accumulators through LDS (both buffers' tiles, which nothing reads any more),
 // 16 bytes a lane next to each other.
@@ -478,9 +479,9 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
 // the r of that product is summed from dS as it was rounded to bf16 for the other (two to an instruction): the part of those
 // roundings that all keys share, which dS itself, summing to 0, does not have, then cancels.
 // p of 1 means a query that sees one key: dS is exactly 0 then, where dP - delta would leave the rounding of two different sums
-// (for dq the correction below comes to exactly 0 by itself where the weight is rounded to 1 and there is no cap).  The rounding of lse leaves p short of 1 by 2^-23 |lse|
-// log2(e), hence the margin; where more keys are visible and one has all but 2^-16 of the weight, the |dS| <= 2^-16 (max dP - min dP)
-// that is left out is a 128th of the rounding of dP's own operands.
+// (for dq the correction below comes to exactly 0 by itself where the weight is rounded to 1 and there is no cap).  The rounding of
+// lse leaves p short of 1 by 2^-23 |lse| log2(e), hence the margin; where more keys are visible and one has all but 2^-16 of the
+// weight, the |dS| <= 2^-16 (max dP - min dP) that is left out is a 128th of the rounding of dP's own operands.
 constexpr float kOneKey = 1.f - 1.f / 65536.f;
 
 template <int DP, int MOD, int SHARE>
