@@ -1,12 +1,15 @@
 // What the kernels of attention under a rule share: their arguments, what a query sees, and the list of the tiles that a
 // workgroup has to visit.
 #pragma once
+#include "attention_choice.h"
 #include "common.h"
 #include "kernels.h"
 
 namespace pt {
 
 constexpr int kRuleTile = 64;            // rows of a streamed tile
+
+inline RuleShape rule_shape(const AttnRuleArgs& g) { return RuleShape{g.nb, g.Sq, g.Sk, g.H, g.Hkv, g.dh, g.order != 0, g.qdoc != nullptr}; }
 
 // more than 64 KB of dynamic LDS has to be asked for, kernel by kernel
 #define PT_RULE_LDS(kernel, bytes)                                                                                          \

@@ -22,8 +22,6 @@
 // forward, 59 dq, 61 dk / dv; 4 x 2048 x 16 packed, prefix, cap 61 / 107 / 89; 1 x 8192 x 16 of 128, causal, 4 key heads, forward
 // 317 (867 TFLOP/s of the visible pairs).  Tiles of 64 rows: two buffers of two take 32 KB at a head size of 64, so four workgroups
 // fit a CU and hide each other's barriers, first loads and lists.
-#include <algorithm>
-
 #include "attention_rules.h"
 
 namespace pt {
@@ -763,39 +761,24 @@ hipError_t launch(K kernel, int blocks, size_t lds, const AttnRuleArgs& g, hipSt
   hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), lds, st, g);
   return hipGetLastError();
 }
-// Blocks of 128 rows, or blocks of 64 with two waves for 32 rows where those of 128 would leave CUs without one.  Measured, blocks of
-// 64 against 128, forward / backward: 1 x 384 rows x 8 heads of 64 9.9 / 24 us against 11.5 / 34; 8 x 663 x 2 heads of 128 20 / 59
-// against 26 / 81.  Ordered rows without documents differ in length by their place, and up to two blocks a CU the smaller blocks even
-// that out: 3 x 2048 x 8 38 / 107 against 45 / 143, 1 x 4096 x 16 69 / 214 against 78 / 264.  So they do for every rule in the forward pass at
-// a head size of 64, whose registers leave room for them (12 x 384 x 10 15 against 16, 2 x 2048 x 12 in documents 22 against 24), but
-// not back: 55 against 49, 72 against 66.  Heads of 128 take them forward for ordered rows (1 x 3441 x 12 81 against 112, but 2 x 2048
-// x 12 in documents 38 against 33); backward only up to one block a CU, where the longest is all that counts (1 x 8192 x 16 on 4 key
-// heads 1760 against 2360, but 1 x 4096 x 16 555 against 430).
-constexpr int kCUs = 256;
-int blocks_of(int groups, int rows, int each) { return groups * ((rows + each - 1) / each); }
-template <int DP>
-bool two_waves(const AttnRuleArgs& g, int whole, bool bwd) {
-  const bool uneven = g.order && !g.qdoc;
-  const bool twice = bwd ? uneven && DP == 64 : uneven || DP == 64;
-  return twice ? whole <= 2 * kCUs : uneven ? whole <= kCUs : whole < kCUs;
-}
+int blocks_of(int heads, int rows, int share) { return (int)rule_blocks(heads, rows, 128 / share); }
 
 template <int DP, int MOD>
 hipError_t launch_fwd(const AttnRuleArgs& g, hipStream_t st) {
-  const int heads = g.nb * g.H, whole = blocks_of(heads, g.Sq, 128);
+  const int heads = g.nb * g.H;
   const size_t lds = lds_bytes<DP>(g.Sk, false);
-  return two_waves<DP>(g, whole, false) ? launch(rule_fwd_kernel<DP, MOD, 2>, blocks_of(heads, g.Sq, 64), lds, g, st)
-                                        : launch(rule_fwd_kernel<DP, MOD, 1>, whole, lds, g, st);
+  return rule_share_fwd(rule_shape(g)) == 2 ? launch(rule_fwd_kernel<DP, MOD, 2>, blocks_of(heads, g.Sq, 2), lds, g, st)
+                                            : launch(rule_fwd_kernel<DP, MOD, 1>, blocks_of(heads, g.Sq, 1), lds, g, st);
 }
 template <int DP, int MOD>
 hipError_t launch_bwd(const AttnRuleArgs& g, hipStream_t st) {
-  const int heads = g.nb * g.H, key_heads = g.nb * g.Hkv, whole_q = blocks_of(heads, g.Sq, 128), whole_k = blocks_of(key_heads, g.Sk, 128);
+  const int heads = g.nb * g.H, key_heads = g.nb * g.Hkv;
   const size_t lds_q = lds_bytes<DP>(g.Sk, false), lds_k = lds_bytes<DP>(g.Sq, true);
-  const hipError_t e = two_waves<DP>(g, whole_q, true) ? launch(rule_dq_kernel<DP, MOD, 2>, blocks_of(heads, g.Sq, 64), lds_q, g, st)
-                                                       : launch(rule_dq_kernel<DP, MOD, 1>, whole_q, lds_q, g, st);
+  const hipError_t e = rule_share_dq(rule_shape(g)) == 2 ? launch(rule_dq_kernel<DP, MOD, 2>, blocks_of(heads, g.Sq, 2), lds_q, g, st)
+                                                         : launch(rule_dq_kernel<DP, MOD, 1>, blocks_of(heads, g.Sq, 1), lds_q, g, st);
   if (e != hipSuccess) return e;
-  return two_waves<DP>(g, whole_k, true) ? launch(rule_dkv_kernel<DP, MOD, 2>, blocks_of(key_heads, g.Sk, 64), lds_k, g, st)
-                                         : launch(rule_dkv_kernel<DP, MOD, 1>, whole_k, lds_k, g, st);
+  return rule_share_dkv(rule_shape(g)) == 2 ? launch(rule_dkv_kernel<DP, MOD, 2>, blocks_of(key_heads, g.Sk, 2), lds_k, g, st)
+                                            : launch(rule_dkv_kernel<DP, MOD, 1>, blocks_of(key_heads, g.Sk, 1), lds_k, g, st);
 }
 template <int DP>
 hipError_t by_mod(const AttnRuleArgs& g, bool bwd, hipStream_t st) {

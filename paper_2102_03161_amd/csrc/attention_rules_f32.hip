@@ -343,12 +343,9 @@ hipError_t launch_shared(const AttnRuleArgs& g, bool bwd, hipStream_t st) {
   else hipLaunchKernelGGL((rule_fwd_f32_kernel<DP, SHARE>), dim3(nq), dim3(256), lds, st, g);
   return hipGetLastError();
 }
-// two waves for 16 rows where workgroups of 64 rows would not be one for each CU
 template <int DP>
 hipError_t launch_f32(const AttnRuleArgs& g, bool bwd, hipStream_t st) {
-  constexpr int kCUs = 256;
-  const int64_t nq = (int64_t)g.nb * g.H * ((g.Sq + 63) / 64), nk = (int64_t)g.nb * g.Hkv * ((g.Sk + 63) / 64);
-  return (bwd ? nq + nk : nq) < kCUs ? launch_shared<DP, 2>(g, bwd, st) : launch_shared<DP, 1>(g, bwd, st);
+  return rule_share_f32(rule_shape(g), bwd) == 2 ? launch_shared<DP, 2>(g, bwd, st) : launch_shared<DP, 1>(g, bwd, st);
 }
 
 }  // namespace
