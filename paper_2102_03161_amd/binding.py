@@ -346,9 +346,10 @@ def attention_backward(q, k, v, o, lse, do, rule: AttentionRule | None = None, g
         out = (*_heads(dq, "dq", qs, dtype), *_heads(dk, "dk", ks, dtype), *_heads(dv, "dv", ks, dtype))
     lib, args = _fast or _fast_library(), _args
     _PACK[8](args.buf, 0, *a, *hq, *hk, *hv, *ho, *hd, *out)
-    ws = _torch.empty_like(lse)      # as many bytes as pt_attention_workspace asks for, which the call checks
+    floats = nb * H * Sq * (2 if dtype is _torch.float32 else 1)      # as many as pt_attention_workspace asks for, which the call checks
+    ws = _torch.empty(floats, dtype=_torch.float32, device=q.device)
     h = args.heads
-    _launch(at, lib.pt_attention_bwd, args.at, h[0], h[1], h[2], h[3], stats, h[4], h[5], h[6], h[7], ws.data_ptr(), 4 * nb * H * Sq)
+    _launch(at, lib.pt_attention_bwd, args.at, h[0], h[1], h[2], h[3], stats, h[4], h[5], h[6], h[7], ws.data_ptr(), 4 * floats)
     return dq, dk, dv
 
 

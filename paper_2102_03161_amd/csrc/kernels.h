@@ -74,7 +74,7 @@ struct AttnRuleArgs {
   const int64_t* bmap;       // sample b's documents and prefix are those of row bmap[b]; null: b
   HeadView q, k, v, o, d_o, dq, dk, dv;
   float* lse; int64_t lse_b, lse_h;   // forward: written unless null; backward: read
-  float* delta;              // backward in bf16: scratch [nb, H, Sq]
+  float* delta;              // backward: scratch [nb, H, Sq], in fp32 two of those
 };
 constexpr int kRuleMaxRows = 1 << 18;   // of queries or keys: the list of tiles lives in LDS
 constexpr int64_t kRuleMaxBlocks = 1 << 23;   // blocks of 64 rows, queries' and keys' together: a launch has fewer than 2^31 threads

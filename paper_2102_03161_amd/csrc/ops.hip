@@ -87,7 +87,8 @@ pt_status pt_attention_workspace(const pt_attention* a, size_t* bwd_bytes) {
   const pt_status s = check_attention(a);
   if (s != PT_OK) return s;
   if (!bwd_bytes) return fail(PT_EINVAL, "bwd_bytes is NULL");
-  *bwd_bytes = a->dtype == PT_BF16 ? (size_t)a->nb * a->H * a->Sq * sizeof(float) : 0;   // delta, which the fp32 kernels keep to themselves
+  // what dq's pass leaves for the keys': delta, and in fp32 another value for each query
+  *bwd_bytes = (size_t)a->nb * a->H * a->Sq * sizeof(float) * (a->dtype == PT_BF16 ? 1 : 2);
   return PT_OK;
 }
 

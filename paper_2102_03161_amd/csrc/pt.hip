@@ -187,7 +187,7 @@ void make_plan(const pt_config& c, Plan* p) {
   p->sA = take(TD4); p->sB = take(TD4); p->sC = take(TD4); p->sD = take(TD4);
   p->oA = take(TD); p->oB = take(TD); p->oC = take(TD); p->oD = take(TD); p->oE = take(TD); p->dF = take(TF);
   p->oE2 = c.arch == PT_BERT_POSTLN ? take(TD) : p->oE;   // post-LN: successive blocks alternate (see block_backward)
-  p->dQKV = take(3 * TD); p->DELTA = take(BHS);
+  p->dQKV = take(3 * TD); p->DELTA = take(c.dtype == PT_F32 ? 2 * BHS : BHS);
   {
     const size_t BD = (size_t)B * D, BF = (size_t)B * F;
     p->rG = take(BF * e); p->rHP = take(BF * e); p->rDF = take(BF * e);

@@ -17,8 +17,9 @@ extern "C" int share(int what, int nb, int Sq, int Sk, int H, int Hkv, int dh, i
     case 0: return rule_share_fwd(s);
     case 1: return rule_share_dq(s);
     case 2: return rule_share_dkv(s);
-    case 3: return rule_share_f32(s, false);
-    default: return rule_share_f32(s, true);
+    case 3: return rule_share_f32_fwd(s);
+    case 4: return rule_share_f32_dq(s);
+    default: return rule_share_f32_dkv(s);
   }
 }
 """
@@ -27,7 +28,7 @@ _lib = None
 
 
 def shares(nb, Sq, Sk, H, Hkv, dh, ordered=False, documents=False, bf16=True):
-    """Waves that share the rows of a wave: (forward, dq, dk and dv) in bf16, (forward, backward) in fp32."""
+    """Waves that share the rows of a wave: (forward, dq, dk and dv)."""
     global _lib
     if _lib is None:
         with tempfile.TemporaryDirectory() as d:
@@ -35,4 +36,4 @@ def shares(nb, Sq, Sk, H, Hkv, dh, ordered=False, documents=False, bf16=True):
             subprocess.run(["g++", "-std=c++17", "-O1", "-fPIC", "-shared", "-I", CSRC, "-x", "c++", "-", "-o", so],
                            input=SOURCE.encode(), check=True)
             _lib = ctypes.CDLL(so)
-    return tuple(_lib.share(what, nb, Sq, Sk, H, Hkv, dh, int(ordered), int(documents)) for what in ((0, 1, 2) if bf16 else (3, 4)))
+    return tuple(_lib.share(what, nb, Sq, Sk, H, Hkv, dh, int(ordered), int(documents)) for what in ((0, 1, 2) if bf16 else (3, 4, 5)))

@@ -25,9 +25,10 @@ def test_bf16_wider_heads():
 
 def test_f32():
     rows = dict(Sq=200, Sk=200, dh=64, bf16=False)            # four blocks of 64 rows a head
-    assert shares(1, H=31, Hkv=31, **rows) == (2, 2)
-    assert shares(1, H=63, Hkv=63, **rows)[0] == 2
-    assert shares(1, H=64, Hkv=64, **rows) == (1, 1)
+    assert shares(1, H=63, Hkv=63, **rows) == (2, 2, 2)
+    assert shares(1, H=64, Hkv=64, **rows) == (1, 2, 2)
+    assert shares(1, H=128, Hkv=64, **rows) == (1, 1, 2)
+    assert shares(1, H=128, Hkv=128, **rows) == (1, 1, 1)
 
 
 def test_counts_that_pass_32_bits():

@@ -23,11 +23,11 @@ BF16_CASES = [
     (9, 333, 20, 20, 96, "full", None, 0.0, False),
 ]
 F32_CASES = [
-    (4, 200, 17, 17, 16, "causal", None, 0.0, True),
-    (4, 200, 17, 17, 64, "full", "packed", 7.0, False),
-    (3, 333, 16, 16, 128, "prefix", "mixed", 0.0, False),
-    (4, 200, 34, 17, 64, "full", "padded", 0.0, True),
-    (4, 200, 17, 17, 104, "causal", "packed", 11.0, True),
+    (8, 200, 17, 17, 16, "causal", None, 0.0, True),
+    (8, 200, 17, 17, 64, "full", "packed", 7.0, False),
+    (6, 333, 16, 16, 128, "prefix", "mixed", 0.0, False),
+    (8, 200, 34, 17, 64, "full", "padded", 0.0, True),
+    (8, 200, 17, 17, 104, "causal", "packed", 11.0, True),
 ]
 
 
