@@ -34,6 +34,7 @@ typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 namespace {
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ uint64_t swapped(uint64_t lanes) { return lanes >> 32 | lanes << 32; }   // the mask of the lanes 32 away
 // the value of the lane 32 away
 __device__ __forceinline__ float half_swap(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -476,11 +477,10 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
 // w_ij k_j), w = p (1 - tanh^2): one more product with the keys' fragments that the pass has in registers anyway.  Without a cap
 // the r of that product is summed from dS as it was rounded to bf16 for the other (two to an instruction): the part of those
 // roundings that all keys share, which dS itself, summing to 0, does not have, then cancels.
-// p of 1 means a query that sees one key: dS is exactly 0 then, where dP - delta would leave the rounding of two different sums
-// (for dq the correction below comes to exactly 0 by itself where the weight is rounded to 1 and there is no cap).  The rounding of
-// lse leaves p short of 1 by 2^-23 |lse| log2(e), hence the margin; where more keys are visible and one has all but 2^-16 of the
-// weight, the |dS| <= 2^-16 (max dP - min dP) that is left out is a 128th of the rounding of dP's own operands.
-constexpr float kOneKey = 1.f - 1.f / 65536.f;
+// A query that sees one key has dS = 0, where dP - delta would leave the rounding of two different sums.  The pass counts the keys that
+// have some weight, in masked tiles (a whole one has several) and only until each of the wave's queries has met two, as lane masks in
+// scalar registers: the kernel has no vector register left.  The keys' pass finds a mark in place of such a query's delta.
+constexpr uint32_t kOneKey = 0x7fc0a11eu;   // a NaN that no operation makes
 
 template <int DP, int MOD, int SHARE>
 __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dq_kernel(AttnRuleArgs g) {
@@ -512,6 +512,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dq_kernel(
 #pragma unroll
   for (int dt = 0; dt < T::DT; ++dt) { dq[dt] = zero16(); wk[dt] = zero16(); }
   float rest = 0.f, rounded = 0.f;   // r, and r from dS as it was rounded
+  uint64_t one = 0, two = __ballot(!on);   // lanes that have met a key of some weight, and another
   const bool few = few_pairs<SHARE>(g);
   auto load = [&](int e, int at) {
     const int j0 = list.tile(e) * kRuleTile;
@@ -556,12 +557,20 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dq_kernel(
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               const int v = 4 * g4 + x;
-              // the correction below is an exact 0 for a query that sees one key only where its weight is rounded to 1
-              if (((MOD & 1) || few) && w[v] >= kOneKey) dp[v] = 0.f;
               w[v] = kd[x] == qd ? w[v] : 0.f;
               if (g.order != 0) w[v] = 32 * st + 8 * g4 + x <= far ? w[v] : 0.f;
             }
           }
+          if (~(two | swapped(two) | (one & swapped(one)))) {   // some query has not met two keys yet
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+              const uint64_t here = __ballot(w[v] != 0.f);
+              two |= one & here;
+              one |= here;
+            }
+          }
+        } else {
+          two = ~0ull;
         }
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
@@ -584,23 +593,27 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dq_kernel(
   }
   rest += half_swap(rest);
   rounded = (MOD & 1) ? rest : rounded + half_swap(rounded);
+  int seen = (int)(one >> lane & 1) + 2 * (int)(two >> lane & 1);
+  seen += __float_as_int(half_swap(__int_as_float(seen)));
   float* room = reinterpret_cast<float*>(smem);
   if (SHARE == 2) {   // r is the sum over both waves' keys, and each takes its own part of the product out with it
-    float* stat = room + group * 256;
+    float* stat = room + group * 384;
     __syncthreads();
-    stat[128 * x0 + lane] = rest;
-    stat[128 * x0 + 64 + lane] = rounded;
+    stat[192 * x0 + lane] = rest;
+    stat[192 * x0 + 64 + lane] = rounded;
+    stat[192 * x0 + 128 + lane] = __int_as_float(seen);
     __syncthreads();
-    const float rest2 = stat[128 * (1 - x0) + lane], rounded2 = stat[128 * (1 - x0) + 64 + lane];
+    const float rest2 = stat[192 * (1 - x0) + lane], rounded2 = stat[192 * (1 - x0) + 64 + lane];
+    seen += __float_as_int(stat[192 * (1 - x0) + 128 + lane]);
     rest = x0 ? rest2 + rest : rest + rest2;
     rounded = x0 ? rounded2 + rounded : rounded + rounded2;
   }
   if (SHARE == 1 && !ok) return;
-  if (ok && x0 == 0 && half == 0) g.delta[((int64_t)b * g.H + h) * g.Sq + i] = on ? dl + rest : 0.f;
+  if (ok && x0 == 0 && half == 0) g.delta[((int64_t)b * g.H + h) * g.Sq + i] = seen == 1 ? __uint_as_float(kOneKey) : on ? dl + rest : 0.f;
 #pragma unroll
   for (int dt = 0; dt < T::DT; ++dt)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) dq[dt][v] = fmaf(-rounded, wk[dt][v], dq[dt][v]);
+    for (int v = 0; v < 16; ++v) dq[dt][v] = seen == 1 ? 0.f : fmaf(-rounded, wk[dt][v], dq[dt][v]);
   if (SHARE == 2) {
     __syncthreads();
     if (x0) leave(room, group, lane, dq);
@@ -714,7 +727,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dkv_kernel
                 for (int x = 0; x < 4; ++x) s[4 * g4 + x] = j <= lm[x] ? s[4 * g4 + x] : 0.f;
               }
 #pragma unroll
-              for (int x = 0; x < 4; ++x) ds[4 * g4 + x] = s[4 * g4 + x] >= kOneKey ? 0.f : ds[4 * g4 + x];
+              for (int x = 0; x < 4; ++x) ds[4 * g4 + x] = __float_as_uint(dl[x]) == kOneKey ? 0.f : ds[4 * g4 + x];
             }
 #pragma unroll
             for (int x = 0; x < 4; ++x) ds[4 * g4 + x] *= s[4 * g4 + x];

@@ -106,9 +106,17 @@ def test_dominant_keys_in_fp32(nb, S, H, dh, cap, alone):
     check(*dominated(nb, S, H, dh, F32, (13.0, 16.0), alone, gen), cap)
 
 
+@pytest.mark.parametrize("alone", [True, False], ids=["two keys", "all keys"])
+@pytest.mark.parametrize("nb,S,H,dh", [(1, 64, 2, 64), (2, 130, 3, 64), (1, 70, 2, 128), (22, 260, 8, 64)])
+def test_dominant_keys_in_bf16(nb, S, H, dh, alone):
+    gen = torch.Generator().manual_seed(S + dh)
+    check(*dominated(nb, S, H, dh, BF16, (11.2, 12.0), alone, gen), 0.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("cap", [0.0, 400.0])
 @pytest.mark.parametrize("nb,S,H,dh", [(1, 64, 2, 64), (1, 150, 2, 128), (24, 150, 24, 64)])
-def test_one_visible_key_of_a_large_score(nb, S, H, dh, cap, dtype=F32):
+def test_one_visible_key_of_a_large_score(nb, S, H, dh, cap, dtype):
     """Scores of 100 and more: lse, and with it the weight of the only key, is off by more than a unit of 1."""
     gen = torch.Generator().manual_seed(dh)
     k, v, do = (torch.randn(nb, S, H, dh, generator=gen).to(dtype) for _ in range(3))
