@@ -359,8 +359,12 @@ PT_API pt_status pt_profile_read(pt_ctx* ctx, int32_t category, double* total_ms
  * .row + head * .head + d]; data 16-byte aligned, strides multiples of 16 bytes
  * (0 for a broadcast input).
  *   dtype PT_BF16: products of bf16 on the matrix cores, everything else fp32,
- * the probabilities and dS rounded to bf16 for the second products.  PT_F32: all
- * in fp32.  Sums are in a fixed order: results do not vary from run to run. */
+ * the probabilities and dS rounded to bf16 for the second products, unless Sq and
+ * Sk are at most 64: then what that rounding leaves out is added by another
+ * product.  PT_F32: all in fp32.  A query that sees one key has no gradient, and
+ * adds none to that key.  Sums are in a fixed order: results do not vary from
+ * run to run; the order, not the precision, may vary with the number of samples
+ * and heads. */
 typedef struct {
   void* data;
   int64_t sample, row, head;   /* strides in elements */

@@ -304,13 +304,8 @@ __device__ __forceinline__ void take(const float* room, int group, int lane, f32
   }
 }
 
-// Weights are rounded to bf16 for the second products, which adds as much error again as the results' own rounding (1.4 times in
-// all), on average over many weights.  Where a sample and head has few pairs, and there are few of those, nothing averages, and what
-// the rounding left out goes through one more product: 3 x 64 rows x 4 heads then take 5.8 / 14.7 us forward / backward, 5.7 / 13.9
-// without; the branch alone costs the longer rows of these grids 1 % forward and up to 4 % backward.
-constexpr int64_t kFewPairs = 4096;
-template <int SHARE>
-__device__ __forceinline__ bool few_pairs(const AttnRuleArgs& g) { return SHARE == 2 && (int64_t)g.Sq * g.Sk <= kFewPairs; }
+// FEW (attention_choice.h): what a weight's rounding to bf16 leaves out.  3 x 64 rows x 4 heads take 5.8 / 14.7 us forward / backward with
+// that product, 5.7 / 13.9 without.
 __device__ __forceinline__ f32x16 left_out(const f32x16& w) {
   f32x16 r;
 #pragma unroll
@@ -322,7 +317,7 @@ __device__ __forceinline__ f32x16 left_out(const f32x16& w) {
 // anything, and moves only when a tile's sum passes 2^40.  So a tile whose rows all have one needs no maximum at all.
 constexpr float kGrown = 1099511627776.f;   // 2^40
 
-template <int DP, int MOD, int SHARE>
+template <int DP, int MOD, int SHARE, bool FEW>
 __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
   constexpr int kRows = 128 / SHARE, NX = 2 / SHARE;   // rows of a workgroup; parts of 32 rows of a tile that a wave takes
@@ -435,7 +430,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
 #pragma unroll
       for (int st = 0; st < NX; ++st) {
         T::add(T::col_addr(kb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, s[st], o);
-        if (few_pairs<SHARE>(g)) T::add(T::col_addr(kb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, left_out(s[st]), o);
+        if (FEW) T::add(T::col_addr(kb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, left_out(s[st]), o);
       }
     }
     if (it + 1 < n) finish(next, (it + 1) & 1);
@@ -482,7 +477,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
 // scalar registers: the kernel has no vector register left.  The keys' pass finds a mark in place of such a query's delta.
 constexpr uint32_t kOneKey = 0x7fc0a11eu;   // a NaN that no operation makes
 
-template <int DP, int MOD, int SHARE>
+template <int DP, int MOD, int SHARE, bool FEW>
 __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dq_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
   constexpr int kRows = 128 / SHARE, NX = 2 / SHARE;   // rows of a workgroup; parts of 32 rows of a tile that a wave takes
@@ -513,7 +508,6 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dq_kernel(
   for (int dt = 0; dt < T::DT; ++dt) { dq[dt] = zero16(); wk[dt] = zero16(); }
   float rest = 0.f, rounded = 0.f;   // r, and r from dS as it was rounded
   uint64_t one = 0, two = __ballot(!on);   // lanes that have met a key of some weight, and another
-  const bool few = few_pairs<SHARE>(g);
   auto load = [&](int e, int at) {
     const int j0 = list.tile(e) * kRuleTile;
     sd.load(j0);
@@ -583,7 +577,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dq_kernel(
           }
         }
         T::add2(T::col_addr(kb, lane) + 32 * x0 * T::RB, 32 * st, dp, dq, w, wk, (MOD & 1) ? nullptr : &rounded);
-        if (few)
+        if (FEW)
           T::add2(T::col_addr(kb, lane) + 32 * x0 * T::RB, 32 * st, left_out(dp), dq, left_out(w), wk, (MOD & 1) ? nullptr : &rounded);
       }
     }
@@ -624,7 +618,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dq_kernel(
   T::put(static_cast<bf16*>(const_cast<void*>(g.dq.p)) + b * g.dq.b + (int64_t)i * g.dq.t + h * g.dq.h, g.dh, half, g.scale, dq);
 }
 
-template <int DP, int MOD, int SHARE>
+template <int DP, int MOD, int SHARE, bool FEW>
 __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dkv_kernel(AttnRuleArgs g) {
   typedef Tile<DP> T;
   constexpr int kRows = 128 / SHARE, NX = 2 / SHARE;   // rows of a workgroup; parts of 32 rows of a tile that a wave takes
@@ -733,11 +727,9 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dkv_kernel
             for (int x = 0; x < 4; ++x) ds[4 * g4 + x] *= s[4 * g4 + x];
           }
           T::add(T::col_addr(qb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, s, dv);
+          if (FEW) T::add(T::col_addr(qb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, left_out(s), dv);
           T::add(T::col_addr(qb, lane) + 32 * x0 * T::RB, 32 * st, ds, dk);
-          if (few_pairs<SHARE>(g)) {
-            T::add(T::col_addr(qb + T::BYTES, lane) + 32 * x0 * T::RB, 32 * st, left_out(s), dv);
-            T::add(T::col_addr(qb, lane) + 32 * x0 * T::RB, 32 * st, left_out(ds), dk);
-          }
+          if (FEW) T::add(T::col_addr(qb, lane) + 32 * x0 * T::RB, 32 * st, left_out(ds), dk);
         }
       }
       if (it + 1 < n) finish(next, (it + 1) & 1);
@@ -776,30 +768,34 @@ hipError_t launch(K kernel, int blocks, size_t lds, const AttnRuleArgs& g, hipSt
 }
 int blocks_of(int heads, int rows, int share) { return (int)rule_blocks(heads, rows, 128 / share); }
 
-template <int DP, int MOD>
+template <int DP, int MOD, int SHARE, bool FEW>
 hipError_t launch_fwd(const AttnRuleArgs& g, hipStream_t st) {
-  const int heads = g.nb * g.H;
-  const size_t lds = lds_bytes<DP>(g.Sk, false);
-  return rule_share_fwd(rule_shape(g)) == 2 ? launch(rule_fwd_kernel<DP, MOD, 2>, blocks_of(heads, g.Sq, 2), lds, g, st)
-                                            : launch(rule_fwd_kernel<DP, MOD, 1>, blocks_of(heads, g.Sq, 1), lds, g, st);
+  return launch(rule_fwd_kernel<DP, MOD, SHARE, FEW>, blocks_of(g.nb * g.H, g.Sq, SHARE), lds_bytes<DP>(g.Sk, false), g, st);
+}
+template <int DP, int MOD, int SHARE, bool FEW>
+hipError_t launch_dq(const AttnRuleArgs& g, hipStream_t st) {
+  return launch(rule_dq_kernel<DP, MOD, SHARE, FEW>, blocks_of(g.nb * g.H, g.Sq, SHARE), lds_bytes<DP>(g.Sk, false), g, st);
+}
+template <int DP, int MOD, int SHARE, bool FEW>
+hipError_t launch_dkv(const AttnRuleArgs& g, hipStream_t st) {
+  return launch(rule_dkv_kernel<DP, MOD, SHARE, FEW>, blocks_of(g.nb * g.Hkv, g.Sk, SHARE), lds_bytes<DP>(g.Sq, true), g, st);
 }
 template <int DP, int MOD>
-hipError_t launch_bwd(const AttnRuleArgs& g, hipStream_t st) {
-  const int heads = g.nb * g.H, key_heads = g.nb * g.Hkv;
-  const size_t lds_q = lds_bytes<DP>(g.Sk, false), lds_k = lds_bytes<DP>(g.Sq, true);
-  const hipError_t e = rule_share_dq(rule_shape(g)) == 2 ? launch(rule_dq_kernel<DP, MOD, 2>, blocks_of(heads, g.Sq, 2), lds_q, g, st)
-                                                         : launch(rule_dq_kernel<DP, MOD, 1>, blocks_of(heads, g.Sq, 1), lds_q, g, st);
+hipError_t launch_all(const AttnRuleArgs& g, bool bwd, hipStream_t st) {
+  const RuleShape s = rule_shape(g);
+  const bool few = rule_few_pairs(s);
+  if (!bwd) return few ? launch_fwd<DP, MOD, 2, true>(g, st) : rule_share_fwd(s) == 2 ? launch_fwd<DP, MOD, 2, false>(g, st) : launch_fwd<DP, MOD, 1, false>(g, st);
+  const hipError_t e = few ? launch_dq<DP, MOD, 2, true>(g, st) : rule_share_dq(s) == 2 ? launch_dq<DP, MOD, 2, false>(g, st) : launch_dq<DP, MOD, 1, false>(g, st);
   if (e != hipSuccess) return e;
-  return rule_share_dkv(rule_shape(g)) == 2 ? launch(rule_dkv_kernel<DP, MOD, 2>, blocks_of(key_heads, g.Sk, 2), lds_k, g, st)
-                                            : launch(rule_dkv_kernel<DP, MOD, 1>, blocks_of(key_heads, g.Sk, 1), lds_k, g, st);
+  return few ? launch_dkv<DP, MOD, 2, true>(g, st) : rule_share_dkv(s) == 2 ? launch_dkv<DP, MOD, 2, false>(g, st) : launch_dkv<DP, MOD, 1, false>(g, st);
 }
 template <int DP>
 hipError_t by_mod(const AttnRuleArgs& g, bool bwd, hipStream_t st) {
   switch ((g.cap > 0.f ? 1 : 0) | (g.slopes ? 2 : 0)) {
-    case 0: return bwd ? launch_bwd<DP, 0>(g, st) : launch_fwd<DP, 0>(g, st);
-    case 1: return bwd ? launch_bwd<DP, 1>(g, st) : launch_fwd<DP, 1>(g, st);
-    case 2: return bwd ? launch_bwd<DP, 2>(g, st) : launch_fwd<DP, 2>(g, st);
-    default: return bwd ? launch_bwd<DP, 3>(g, st) : launch_fwd<DP, 3>(g, st);
+    case 0: return launch_all<DP, 0>(g, bwd, st);
+    case 1: return launch_all<DP, 1>(g, bwd, st);
+    case 2: return launch_all<DP, 2>(g, bwd, st);
+    default: return launch_all<DP, 3>(g, bwd, st);
   }
 }
 

@@ -23,6 +23,12 @@ def test_bf16_wider_heads():
     assert shares(1, H=257, Hkv=257, ordered=True, **rows) == (1, 1, 1)
 
 
+def test_few_pairs_whatever_the_batch():
+    for nb in (1, 1000):
+        assert shares(nb, 64, 64, 12, 12, 64) == shares(nb, 1, 64, 12, 3, 128) == (2, 2, 2)
+    assert shares(1000, 65, 64, 12, 12, 64) == shares(1000, 64, 65, 12, 12, 64) == (1, 1, 1)
+
+
 def test_f32():
     rows = dict(Sq=200, Sk=200, dh=64, bf16=False)            # four blocks of 64 rows a head
     assert shares(1, H=63, Hkv=63, **rows) == (2, 2, 2)
