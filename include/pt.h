@@ -143,7 +143,8 @@ PT_API pt_status pt_get_freeze_boundary(const pt_ctx* ctx, int32_t* k /*HOST out
  * PT_EINVAL).  Cached rows are those of the rule that they were written under: the caller keeps it the same per sample.
  * Padding (documents below 0) takes no part in attention; the span head leaves it out of the softmax over the sequence,
  * and a label on it has loss 0 and no gradient.  Everything else (positions, LayerNorm, MLP) is per token and unchanged.
- * PT_ESTATE between pt_frozen_forward and pt_active_fwd_bwd of a batch. */
+ * PT_ESTATE between pt_frozen_forward and pt_active_fwd_bwd of a batch; behind them, the batch can be updated from but
+ * not run again (pt_active_fwd_bwd is PT_ESTATE until the next pt_frozen_forward). */
 typedef struct {
   int32_t order;              /* PT_ATTN_*                                     */
   int32_t n;                  /* samples that documents and prefix describe    */

@@ -278,6 +278,7 @@ struct pt_ctx {
   int nb = 0;
   void* last_hk = nullptr;
   struct { bool on = false, slopes = false, docs = false, prefix = false; int order = 0, n = 0; float cap = 0.f; } rule;   // pt_set_attention
+  bool rule_new = false;               // the rule was set since the last frozen forward
   const int64_t* rule_map = nullptr;   // device: sample of the caller's batch that position b of the blocks' batch is; null: b
   hipError_t op_err = hipSuccess;      // first failed launch of an operator since the last check
   void* last_dhk = nullptr;
@@ -1075,7 +1076,7 @@ pt_status pt_set_freeze_boundary(pt_ctx* c, int32_t k) {
 pt_status pt_set_attention(pt_ctx* c, const pt_attention_rule* r) {
   if (!c) return PT_EINVAL;
   if (c->phase == 1) return fail(c, PT_ESTATE, "the attention rule cannot change between a batch's forward and backward pass");
-  if (!r) { c->rule = {}; return PT_OK; }
+  if (!r) { c->rule = {}; c->rule_new = true; return PT_OK; }
   const pt_config& g = c->cfg;
   const Plan& p = c->plan;
   if (r->order != PT_ATTN_FULL && r->order != PT_ATTN_CAUSAL && r->order != PT_ATTN_PREFIX) return fail(c, PT_EINVAL, "order");
@@ -1086,6 +1087,7 @@ pt_status pt_set_attention(pt_ctx* c, const pt_attention_rule* r) {
   if (r->documents) HIP_TRY(c, hipMemcpyAsync(c->w(p.DOCS), r->documents, (size_t)r->n * g.S * 4, hipMemcpyDeviceToDevice, c->st));
   if (r->order == PT_ATTN_PREFIX) HIP_TRY(c, hipMemcpyAsync(c->w(p.PREFIX), r->prefix, (size_t)r->n * 4, hipMemcpyDeviceToDevice, c->st));
   if (r->slopes) HIP_TRY(c, hipMemcpyAsync(c->w(p.SLOPES), r->slopes, (size_t)g.H * 4, hipMemcpyDeviceToDevice, c->st));
+  c->rule_new = true;
   c->rule.on = true;
   c->rule.order = r->order;
   c->rule.cap = r->cap;
@@ -1391,6 +1393,7 @@ pt_status pt_frozen_forward(pt_ctx* c, const void* d_input, int32_t nb, const in
   HIP_TRY(c, hipGetLastError());
   c->nb = nb;
   c->phase = 1;
+  c->rule_new = false;
   *d_hk_out = c->last_hk;
   return PT_OK;
 }
@@ -1425,6 +1428,7 @@ pt_status pt_time_frozen_forward(pt_ctx* c, const void* d_input, int32_t nb, con
 pt_status pt_active_fwd_bwd(pt_ctx* c, const void* d_hk, const int32_t* d_labels, float* loss_out) {
   if (!c || !d_hk || !d_labels) return PT_EINVAL;
   if (c->phase < 1) return fail(c, PT_ESTATE, "pt_frozen_forward has not run for this step");
+  if (c->rule_new) return fail(c, PT_ESTATE, "the attention rule was set behind this batch's pt_frozen_forward");
   if (reinterpret_cast<uintptr_t>(d_hk) % 16) return fail(c, PT_EINVAL, "d_hk must be 16-byte aligned");
   { const pt_status fs = flush_deferred_norms(c); if (fs != PT_OK) return fs; }   // pending norms are of the gradients and boundary as they are now
   c->ln_jobs.clear();
