@@ -140,7 +140,9 @@ PT_API pt_status pt_get_freeze_boundary(const pt_ctx* ctx, int32_t* k /*HOST out
  * pt_frozen_forward on; rule NULL: plain attention again.  For padded batches, packed rows and prefix or causal models.
  * The arrays are copied on the context's stream: slopes for good, documents and prefix lengths for batches whose sample
  * b they describe in row b (the caller sets them again for a batch with others; a batch of more than n samples is
- * PT_EINVAL).  Cached rows are those of the rule that they were written under: the caller keeps it the same per sample.
+ * PT_EINVAL).  A rule of another order or cap, or with slopes where there were none (or the reverse; NULL is PT_ATTN_FULL
+ * without either), empties the activation cache.  Within one of those, cached rows are those of the slopes, documents and
+ * prefix that they were written under: the caller keeps them the same per sample.
  * Padding (documents below 0) takes no part in attention; the span head leaves it out of the softmax over the sequence,
  * and a label on it has loss 0 and no gradient.  Everything else (positions, LayerNorm, MLP) is per token and unchanged.
  * PT_ESTATE between pt_frozen_forward and pt_active_fwd_bwd of a batch; behind them, the batch can be updated from but

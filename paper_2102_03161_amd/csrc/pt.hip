@@ -1073,10 +1073,26 @@ pt_status pt_set_freeze_boundary(pt_ctx* c, int32_t k) {
   return PT_OK;
 }
 
+// A rule's order, cap and having slopes make another model of the prefix: cached rows of the old one are dropped, staged ones too (their
+// window slots are free like evicted ones).
+static void set_rule_shape(pt_ctx* c, int order, float cap, bool slopes) {
+  if (order != c->rule.order || cap != c->rule.cap || slopes != c->rule.slopes) {
+    std::fill(c->slot_k.begin(), c->slot_k.end(), -1);
+    c->win_of.clear();
+    for (auto& w : c->win)
+      if (w.state == 1) { w.state = 0; w.id = -1; }
+  }
+  c->rule = {};
+  c->rule.order = order;
+  c->rule.cap = cap;
+  c->rule.slopes = slopes;
+  c->rule_new = true;
+}
+
 pt_status pt_set_attention(pt_ctx* c, const pt_attention_rule* r) {
   if (!c) return PT_EINVAL;
   if (c->phase == 1) return fail(c, PT_ESTATE, "the attention rule cannot change between a batch's forward and backward pass");
-  if (!r) { c->rule = {}; c->rule_new = true; return PT_OK; }
+  if (!r) { set_rule_shape(c, PT_ATTN_FULL, 0.f, false); return PT_OK; }
   const pt_config& g = c->cfg;
   const Plan& p = c->plan;
   if (r->order != PT_ATTN_FULL && r->order != PT_ATTN_CAUSAL && r->order != PT_ATTN_PREFIX) return fail(c, PT_EINVAL, "order");
@@ -1087,12 +1103,9 @@ pt_status pt_set_attention(pt_ctx* c, const pt_attention_rule* r) {
   if (r->documents) HIP_TRY(c, hipMemcpyAsync(c->w(p.DOCS), r->documents, (size_t)r->n * g.S * 4, hipMemcpyDeviceToDevice, c->st));
   if (r->order == PT_ATTN_PREFIX) HIP_TRY(c, hipMemcpyAsync(c->w(p.PREFIX), r->prefix, (size_t)r->n * 4, hipMemcpyDeviceToDevice, c->st));
   if (r->slopes) HIP_TRY(c, hipMemcpyAsync(c->w(p.SLOPES), r->slopes, (size_t)g.H * 4, hipMemcpyDeviceToDevice, c->st));
-  c->rule_new = true;
+  set_rule_shape(c, r->order, r->cap, r->slopes != nullptr);
   c->rule.on = true;
-  c->rule.order = r->order;
-  c->rule.cap = r->cap;
   c->rule.n = r->n;
-  c->rule.slopes = r->slopes != nullptr;
   c->rule.docs = r->documents != nullptr;
   c->rule.prefix = r->order == PT_ATTN_PREFIX;
   return PT_OK;

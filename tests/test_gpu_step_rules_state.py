@@ -4,6 +4,7 @@ import pytest
 
 from paper_2102_03161_amd import binding, synth
 from tests import gpu_harness as H
+from tests.test_gpu_parity import MID_BERT
 
 pytestmark = pytest.mark.gpu
 
@@ -37,4 +38,41 @@ def test_a_rule_set_behind_a_pass_waits_for_the_next_batch():
     ctx.optimizer_step(lr=1e-3)
     ruled = ctx.active_fwd_bwd(ctx.frozen_forward(dx), dy)
     assert np.isfinite(ruled) and ruled != plain
+    ctx.close()
+
+
+@pytest.mark.parametrize("host", [False, True], ids=["device rows", "host rows"])
+def test_cached_rows_do_not_outlive_their_order_or_cap(host):
+    import torch
+    w = dict(MID_BERT, dtype="f32")
+    rows = dict(cache_slots=0, host_slots=w["B"], window_slots=2 * w["B"]) if host else dict(cache_slots=w["B"])
+    ctx = context(w, 2, **rows)
+    x, y = H.batch_for(w, 2, w["B"])
+    dx, dy, ids = H.to_dev(torch, x), H.to_dev(torch, y), np.arange(w["B"])
+    slopes = torch.full((w["H"],), 0.1, device="cuda")
+    docs = torch.zeros(w["B"], w["S"], dtype=torch.int32, device="cuda")
+
+    def hk(rule):
+        ctx.set_freeze_boundary(2)
+        ctx.cache_prefetch(ids)
+        ctx.set_attention(rule)
+        ptr = ctx.frozen_forward(dx, ids)
+        out = ctx.read_activation(binding.ACT_HK, (w["B"], w["S"], w["D"]))
+        ctx.active_fwd_bwd(ptr, dy)
+        return out
+
+    rules = [None, binding.AttentionRule(order="causal"), binding.AttentionRule(order="causal", cap=5.0), binding.AttentionRule(cap=5.0, slopes=slopes), None]
+    for n, rule in enumerate(rules):
+        fresh = context(w, 2)
+        fresh.set_attention(rule)
+        fresh.set_freeze_boundary(2)
+        fresh.frozen_forward(dx)
+        want = fresh.read_activation(binding.ACT_HK, (w["B"], w["S"], w["D"]))
+        fresh.close()
+        assert np.array_equal(hk(rule), want), n
+        assert ctx.cache_stats()["misses"] == (n + 1) * w["B"]
+        assert np.array_equal(hk(rule), want), n                     # the same rule again: hits
+        assert ctx.cache_stats()["hits"] == (n + 1) * w["B"]
+    assert np.array_equal(hk(binding.AttentionRule(documents=docs)), want)      # documents are the caller's to keep, sample by sample
+    assert ctx.cache_stats()["hits"] == (len(rules) + 1) * w["B"]
     ctx.close()
