@@ -441,7 +441,8 @@ class Context:
 
     def set_attention(self, rule: AttentionRule | None):
         """Attention of every block under `rule` (its scale and q0 are the context's own: 1 / sqrt(D / H) and 0), from the next
-        batch on; None: plain attention.  documents [n, S] and prefix [n] describe the batches' samples by position."""
+        batch on; None: plain attention.  documents [n, S] and prefix [n] describe the batches' samples by position.  The tensors may be
+        temporaries of the current stream, whichever stream the context works on."""
         if rule is None:
             self._chk(self.lib.pt_set_attention(self.h, None))
             return
@@ -462,6 +463,12 @@ class Context:
         for t in (rule.slopes, *given):
             if t is not None and t.device != self.arenas[0].device:
                 _refuse(f"a tensor on {t.device}, the context on {self.arenas[0].device}")
+        here = _torch.cuda.current_stream(self.device)
+        if here != self.stream:     # the copies wait for what made the tensors, and the tensors' memory for the copies
+            self.stream.wait_stream(here)
+            for t in (rule.slopes, *given):
+                if t is not None:
+                    t.record_stream(self.stream)
         self._chk(self.lib.pt_set_attention(self.h, r))
 
     def frozen_forward(self, d_input, sample_ids=None) -> int:

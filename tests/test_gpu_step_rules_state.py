@@ -76,3 +76,41 @@ def test_cached_rows_do_not_outlive_their_order_or_cap(host):
     assert np.array_equal(hk(binding.AttentionRule(documents=docs)), want)      # documents are the caller's to keep, sample by sample
     assert ctx.cache_stats()["hits"] == (len(rules) + 1) * w["B"]
     ctx.close()
+
+
+def test_a_rule_of_temporaries_on_another_stream():
+    """The context works on a stream of its own, which is behind; the rule's tensors are made late on the caller's, and their memory
+    is used again at once."""
+    import torch
+    w = dict(MID_BERT, dtype="f32")
+    side = torch.cuda.Stream()
+    ctx = binding.Context(binding.make_config(w), stream=side)
+    H.load_params(ctx, H.init_values(w, ctx, 3))
+    x, y = H.batch_for(w, 3, w["B"])
+    dx, dy = H.to_dev(torch, x), H.to_dev(torch, y)
+    docs = (torch.arange(w["S"], device="cuda") // 9).int().repeat(w["B"], 1)
+    slopes, prefix = torch.linspace(0.0, 0.3, w["H"], device="cuda"), torch.arange(w["B"], device="cuda").int() * 7
+    load = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+
+    def loss():
+        out = ctx.active_fwd_bwd(ctx.frozen_forward(dx), dy)
+        torch.cuda.synchronize()
+        return out
+
+    ctx.set_attention(binding.AttentionRule(order="prefix", documents=docs, slopes=slopes, prefix=prefix))
+    torch.cuda.synchronize()
+    want = loss()
+    ctx.set_attention(None)
+    assert loss() != want
+    for busy in (side, torch.cuda.current_stream()):
+        ctx.set_attention(None)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(busy):
+            for _ in range(20):
+                load @ load
+        ctx.set_attention(binding.AttentionRule(order="prefix", documents=docs + 0, slopes=slopes * 1.0, prefix=prefix + 0))
+        waste = [torch.full_like(t, 3) for t in (docs, slopes, prefix) for _ in range(3)]
+        assert loss() == want
+        del waste
+    ctx.close()
