@@ -84,6 +84,7 @@ hipError_t attention_rule_bf16(const AttnRuleArgs& g, bool bwd, hipStream_t st);
 hipError_t attention_rule_f32(const AttnRuleArgs& g, bool bwd, hipStream_t st);
 
 // ---- GELU with an 8-bit checkpoint of its input (format: gelu8.hip); rows of F % 4 == 0 values; dh may be dg, g may be null
+inline int64_t gelu8_max_rows(int F) { return ((int64_t)1 << 27) / ((F + 31) / 32); }   // the kernels count pieces of 4 values in 32 bits
 hipError_t gelu8_fwd(int dt, const void* h, void* g, int8_t* codes, uint8_t* exps, int64_t rows, int F, hipStream_t st);
 hipError_t gelu8_bwd(int dt, const int8_t* codes, const uint8_t* exps, const void* dg, void* dh, void* g, int64_t rows, int F, hipStream_t st);
 

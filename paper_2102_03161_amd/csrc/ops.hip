@@ -73,7 +73,7 @@ AttnRuleArgs rule_args(const pt_attention* a) {
 pt_status check_gelu8(int32_t dtype, int64_t rows, int32_t F) {
   if (dtype != PT_F32 && dtype != PT_BF16) return fail(PT_EINVAL, "dtype");
   if (rows < 0 || F < 4 || F % 4) return fail(PT_EINVAL, "rows >= 0, F a positive multiple of 4");
-  if (rows > ((int64_t)1 << 27) / ((F + 31) / 32)) return fail(PT_EINVAL, "more than 2^27 blocks of 32 values");   // the kernels count pieces of 4 in 32 bits
+  if (rows > gelu8_max_rows(F)) return fail(PT_EINVAL, "more than 2^27 blocks of 32 values");
   return PT_OK;
 }
 

@@ -94,6 +94,7 @@ bool validate(const pt_config& c, std::string* why) {
   if (c.k_min < 0 || c.k_min > c.L) return bad("k_min outside 0..L");
   if (c.act8 != 0 && c.act8 != 1) return bad("act8 is 0 or 1");
   if ((int64_t)c.B * c.S > (1 << 24)) return bad("B*S too large");
+  if (c.act8 && (int64_t)c.B * c.S > gelu8_max_rows(c.F)) return bad("B*S*F too large for 8-bit checkpoints");
   // sequence length: the supported range of the fp32 kernels; the first-token kernels keep a score row of the sequence in LDS
   constexpr size_t kLdsPerCu = 160 * 1024;
   if (!attention_uses_mfma(c.dtype == PT_BF16 ? 1 : 0, dh) && c.S > attention_f32_max_tokens(dh))
