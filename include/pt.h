@@ -95,7 +95,9 @@ typedef struct {
   int32_t act8;        /* 1: active blocks keep their GELU's input as an 8-bit checkpoint (pt_gelu8_fwd) instead of the
                           activation and its derivative: 1 F bytes a token and block in place of 4 F in PT_BF16 mode.  The
                           backward pass takes both from the checkpoint, so gradients carry its rounding; the loss does
-                          not.  The top block under a first-token head keeps its few rows as ever           */
+                          not.  In PT_BF16 mode the GELU's input and its output's gradient also pass through memory, in
+                          bf16, where the step without checkpoints has them in fp32: one rounding more each, the former
+                          in the loss too.  The top block under a first-token head keeps its few rows as ever      */
   int64_t cache_slots; /* 0 = no cache; slot i belongs to sample id i                */
   int64_t host_slots;  /* rows of the host tier: sample ids cache_slots .. cache_slots+host_slots-1 (0 = none) */
   int64_t window_slots;/* device rows the host tier is staged through, >= 2 B when host_slots > 0; they are
