@@ -111,14 +111,15 @@ struct RuleList {
   static __device__ __forceinline__ bool whole(int e, int wave) { return e >> (4 + wave) & 1; }
   static __device__ __forceinline__ bool plain(int e) { return e >> 8 & 1; }
 
-  // raw: the lane's document (below 0: padding); in: it is of a row that exists
+  // raw: the lane's document (below 0: padding); in: it is of a row that exists.  Rows of which none has a document get a range that
+  // ends before it begins, and meet no other (but one from 0 to the largest id, and there pair by pair nothing is visible).
   __device__ __forceinline__ void range(int* lo_, int* hi_, int raw, bool in, int lane) const {
     const bool on = in && raw >= 0;
     const int least = rule_wave_min(on ? raw : 0x7fffffff), most = rule_wave_max(on ? raw : -1);
     const bool pad = __any(in && !on), mixed = least != most || pad;
     if (lane == 0) {
       *lo_ = pad ? least | (int)0x80000000 : least;
-      *hi_ = mixed ? most | (int)0x80000000 : most;
+      *hi_ = mixed ? (most < 0 ? 0 : most) | (int)0x80000000 : most;
     }
   }
   // KEYS: tiles of keys for a block of queries, else tiles of queries for a block of keys; own: the lane's row's document.

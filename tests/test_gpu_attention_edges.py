@@ -4,7 +4,7 @@ import torch
 
 from paper_2102_03161_amd import binding
 from tests.rule_reference import check, reference
-from tests.test_gpu_attention_rules import BF16, F32, both, inputs
+from tests.test_gpu_attention_rules import BF16, F32, both, compare, inputs
 
 pytestmark = pytest.mark.gpu
 TYPES = pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
@@ -27,3 +27,40 @@ def test_a_sample_alone_and_among_others(dtype, order, S):
     want = reference(q[one], k[one], v[one], do[one], few=dtype == BF16, **rule)
     for name in want:
         check(name, whole[name][one], want[name])
+
+
+@TYPES
+def test_padding_against_padding_costs_nothing(dtype):
+    """Rows that are nearly all padding take a fraction of the time of full ones (a 64th of the pairs squared, and the list)."""
+    nb, S, H = 4, 4096, 8
+    gen = torch.Generator().manual_seed(5)
+    q, k, v, do = inputs(nb, S, S, H, H, 64, dtype, gen)
+    docs = torch.zeros(nb, S, dtype=torch.int32, device="cuda")
+    few = docs.clone()
+    few[:, 64:] = -1
+
+    def least(rule):
+        times = []
+        for _ in range(5):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            o, lse = binding.attention_forward(q, k, v, rule)
+            binding.attention_backward(q, k, v, o, lse, do, rule)
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+
+    full, padded = least(binding.AttentionRule(documents=docs)), least(binding.AttentionRule(documents=few))
+    print(f"full rows {full * 1e3:.0f} us, one tile of each {padded * 1e3:.0f} us", flush=True)
+    assert padded < full / 3
+
+
+def test_documents_of_the_largest_id():
+    gen = torch.Generator().manual_seed(6)
+    q, k, v, do = inputs(2, 200, 200, 2, 2, 64, BF16, gen)
+    docs = torch.full((2, 200), (1 << 31) - 1, dtype=torch.int32)
+    docs[0, 60:] = -1
+    docs[1, 100:] = 0
+    docs[1, 130:] = -(1 << 31)
+    compare(q, k, v, do, docs)
