@@ -80,7 +80,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_fwd_f32_kernel(Attn
   A::own(static_cast<const float*>(g.q.p) + b * g.q.b + h * g.q.h, g.q.t, on ? i : g.Sq, g.Sq, g.dh, gr, 1.f, q);
 #pragma unroll
   for (int x = 0; x < A::NF; ++x) o[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -1e30f, sum = 0.f;
+  float m = -INFINITY, sum = 0.f;   // the largest score of a visible pair so far
   int rd = 0;
   auto load = [&](int it) {
     const int j0 = list.tile(list.entry(it)) * kRuleTile;
@@ -113,7 +113,8 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_fwd_f32_kernel(Attn
     }
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float alpha = __builtin_amdgcn_exp2f(m - mx);
+    const float ref = mx == -INFINITY ? 0.f : mx;   // nothing visible yet: any finite reference will do
+    const float alpha = __builtin_amdgcn_exp2f(m - ref);
     m = mx;
     sum *= alpha;
 #pragma unroll
@@ -122,7 +123,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_fwd_f32_kernel(Attn
     for (int x = 0; x < NX; ++x) {
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        s[x][v] = __builtin_amdgcn_exp2f(s[x][v] - mx);
+        s[x][v] = __builtin_amdgcn_exp2f(s[x][v] - ref);
         sum += s[x][v];
       }
       A::add(ys, 16 * (x0 + x), l, gr, s[x], o);
@@ -142,15 +143,16 @@ __global__ __launch_bounds__(256, DP > 64 ? 1 : 2) void rule_fwd_f32_kernel(Attn
     __syncthreads();
     if (part == 1) return;
     const float m2 = at[4 * A::NF], sum2 = at[4 * A::NF + 1], top = fmaxf(m, m2);
-    const float f = __builtin_amdgcn_exp2f(m - top), f2 = __builtin_amdgcn_exp2f(m2 - top);
+    const float ref = top == -INFINITY ? 0.f : top;
+    const float f = __builtin_amdgcn_exp2f(m - ref), f2 = __builtin_amdgcn_exp2f(m2 - ref);
 #pragma unroll
     for (int x = 0; x < A::NF; ++x) o[x] = o[x] * f + *reinterpret_cast<const f32x4*>(at + 4 * x) * f2;
     sum = sum * f + sum2 * f2;
     m = top;
   }
   if (!ok) return;
-  A::put(static_cast<float*>(const_cast<void*>(g.o.p)) + b * g.o.b + (int64_t)i * g.o.t + h * g.o.h, g.dh, gr, sum > 0.f ? 1.f / sum : 0.f, o);
-  if (g.lse && gr == 0) g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i] = sum > 0.f ? (m + log2f(sum)) * 0.693147180559945f : -INFINITY;
+  A::put(static_cast<float*>(const_cast<void*>(g.o.p)) + b * g.o.b + (int64_t)i * g.o.t + h * g.o.h, g.dh, gr, sum == 0.f ? 0.f : 1.f / sum, o);
+  if (g.lse && gr == 0) g.lse[(int64_t)b * g.lse_b + (int64_t)h * g.lse_h + i] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.693147180559945f;
 }
 
 // a += a of the second wave that shares the rows; false in that second wave, which has no more to do

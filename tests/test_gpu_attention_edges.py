@@ -64,3 +64,35 @@ def test_documents_of_the_largest_id():
     docs[1, 100:] = 0
     docs[1, 130:] = -(1 << 31)
     compare(q, k, v, do, docs)
+
+
+@TYPES
+@pytest.mark.parametrize("S", [5, 200])
+def test_scores_far_below_zero(dtype, S):
+    """Every score about -1e31: the only key that a query sees still has all of its weight."""
+    gen = torch.Generator().manual_seed(3)
+    q, k, v, do = inputs(1, S, S, 2, 2, 64, dtype, gen)
+    q, k = torch.full_like(q, 2.0 ** 50), torch.full_like(k, -(2.0 ** 50))
+    docs = torch.arange(S, dtype=torch.int32).view(1, S)
+    rule = binding.AttentionRule(documents=docs.cuda())
+    o, lse = binding.attention_forward(q, k, v, rule)
+    assert torch.equal(o, v)
+    assert ((lse.double() + 8 * 2.0 ** 100).abs() <= 2.0 ** -21 * 8 * 2.0 ** 100).all()    # -64 2^100 / sqrt(64)
+
+
+@TYPES
+@pytest.mark.parametrize("S", [5, 200])
+def test_a_nan_stays_visible(dtype, S):
+    """A row of NaN is no row that sees nothing: its statistic and its gradient say so, the other rows have theirs."""
+    gen = torch.Generator().manual_seed(4)
+    q, k, v, do = (x.clone() for x in inputs(1, S, S, 2, 2, 64, dtype, gen))
+    clean = both(q, k, v, do)
+    q[:, 3] = float("nan")
+    got = both(q, k, v, do)
+    rest = torch.arange(S) != 3
+    for name in ("o", "dq"):
+        assert torch.isnan(got[name][:, 3]).all(), name
+        assert torch.equal(got[name][:, rest], clean[name][:, rest]), name
+    assert torch.isnan(got["lse"][:, :, 3]).all()
+    assert torch.equal(got["lse"][:, :, rest], clean["lse"][:, :, rest])
+    assert torch.isnan(got["dk"]).all() and torch.isnan(got["dv"]).all()
