@@ -37,7 +37,7 @@ struct RuleRows {
   }
   __device__ __forceinline__ int lim(const AttnRuleArgs& g, int i) const {
     if (g.order == 0) return g.Sk - 1;
-    const int at = g.q0 + i, to = at > prefix - 1 ? at : prefix - 1;
+    const int at = g.q0 + i, to = at >= prefix ? at : prefix - 1;   // (the prefix may be any int)
     return to < g.Sk - 1 ? to : g.Sk - 1;
   }
   // as they stand in memory (below 0 behind the last row): nothing looks at the value, so that a load for a later tile is not

@@ -96,3 +96,12 @@ def test_a_nan_stays_visible(dtype, S):
     assert torch.isnan(got["lse"][:, :, 3]).all()
     assert torch.equal(got["lse"][:, :, rest], clean["lse"][:, :, rest])
     assert torch.isnan(got["dk"]).all() and torch.isnan(got["dv"]).all()
+
+
+@TYPES
+def test_prefix_lengths_of_any_value(dtype):
+    """A prefix of no or negative length shows nothing more, one behind the end everything."""
+    gen = torch.Generator().manual_seed(1)
+    lengths = torch.tensor([-(1 << 31), -(1 << 31) + 1, -1, 0, 1, 70, 90, (1 << 31) - 1], dtype=torch.int32)
+    q, k, v, do = inputs(len(lengths), 90, 90, 2, 1, 64, dtype, gen)
+    compare(q, k, v, do, order="prefix", prefix=lengths)
