@@ -147,6 +147,8 @@ PT_API pt_status pt_get_freeze_boundary(const pt_ctx* ctx, int32_t* k /*HOST out
  * prefix that they were written under: the caller keeps them the same per sample.
  * Padding (documents below 0) takes no part in attention; the span head leaves it out of the softmax over the sequence,
  * and a label on it has loss 0 and no gradient.  Everything else (positions, LayerNorm, MLP) is per token and unchanged.
+ * In PT_BF16 mode every head size is computed as pt_attention_fwd says, probabilities and dS rounded to bf16 (without a
+ * rule, head sizes other than 64 keep both in fp32).
  * PT_ESTATE between pt_frozen_forward and pt_active_fwd_bwd of a batch; behind them, the batch can be updated from but
  * not run again (pt_active_fwd_bwd is PT_ESTATE until the next pt_frozen_forward). */
 typedef struct {
@@ -362,7 +364,8 @@ PT_API pt_status pt_profile_read(pt_ctx* ctx, int32_t category, double* total_ms
  * have no gradient.
  *   Views: element (sample, row, head, d) is at data[sample * .sample + row *
  * .row + head * .head + d]; data 16-byte aligned, strides multiples of 16 bytes
- * (0 for a broadcast input).
+ * (0 for a broadcast input; of at least dh for an output, whose elements must not
+ * lie on top of each other).
  *   dtype PT_BF16: products of bf16 on the matrix cores, everything else fp32,
  * the probabilities and dS rounded to bf16 for the second products, unless Sq and
  * Sk are at most 64: then what that rounding leaves out is added by another

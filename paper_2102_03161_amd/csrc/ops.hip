@@ -26,16 +26,16 @@ pt_status launched(hipError_t e) { return e == hipSuccess ? PT_OK : fail(PT_EDEV
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
-// a view of n0 samples, n1 rows, n2 heads; rows are moved in pieces of 16 bytes
-pt_status check_view(const char* name, const pt_heads* v, int64_t n0, int64_t n1, int64_t n2, int dtype, bool written) {
+// a view of n0 samples, n1 rows, n2 heads; rows are moved in pieces of 16 bytes.  written: the dh values of a row and head are its own
+pt_status check_view(const char* name, const pt_heads* v, int64_t n0, int64_t n1, int64_t n2, const pt_attention* a, bool written) {
   if (!v) return fail(PT_EINVAL, "%s is NULL", name);
   if (n0 == 0 || n1 == 0 || n2 == 0) return PT_OK;
   if (!v->data) return fail(PT_EINVAL, "%s: data is NULL", name);
   if (!aligned16(v->data)) return fail(PT_EINVAL, "%s: data must be 16-byte aligned", name);
-  const int64_t m = dtype == PT_BF16 ? 8 : 4, st[3] = {v->sample, v->row, v->head}, n[3] = {n0, n1, n2};
+  const int64_t m = a->dtype == PT_BF16 ? 8 : 4, st[3] = {v->sample, v->row, v->head}, n[3] = {n0, n1, n2};
   for (int i = 0; i < 3; ++i) {
     if (n[i] > 1 && st[i] % m) return fail(PT_EINVAL, "%s: strides must be multiples of %d elements", name, (int)m);
-    if (written && n[i] > 1 && st[i] == 0) return fail(PT_EINVAL, "%s is written: its strides must not be 0", name);
+    if (written && n[i] > 1 && st[i] > -a->dh && st[i] < a->dh) return fail(PT_EINVAL, "%s is written: its strides must be at least the head size", name);
   }
   return PT_OK;
 }
@@ -95,10 +95,10 @@ pt_status pt_attention_workspace(const pt_attention* a, size_t* bwd_bytes) {
 pt_status pt_attention_fwd(const pt_attention* a, const pt_heads* q, const pt_heads* k, const pt_heads* v, const pt_heads* o, float* lse,
                            void* hip_stream) {
   pt_status s = check_attention(a);
-  if (s == PT_OK) s = check_view("q", q, a->nb, a->Sq, a->H, a->dtype, false);
-  if (s == PT_OK) s = check_view("k", k, a->nb, a->Sk, a->Hkv, a->dtype, false);
-  if (s == PT_OK) s = check_view("v", v, a->nb, a->Sk, a->Hkv, a->dtype, false);
-  if (s == PT_OK) s = check_view("o", o, a->nb, a->Sq, a->H, a->dtype, true);
+  if (s == PT_OK) s = check_view("q", q, a->nb, a->Sq, a->H, a, false);
+  if (s == PT_OK) s = check_view("k", k, a->nb, a->Sk, a->Hkv, a, false);
+  if (s == PT_OK) s = check_view("v", v, a->nb, a->Sk, a->Hkv, a, false);
+  if (s == PT_OK) s = check_view("o", o, a->nb, a->Sq, a->H, a, true);
   if (s != PT_OK) return s;
   if (a->nb == 0 || a->Sq == 0) return PT_OK;
   AttnRuleArgs g = rule_args(a);
@@ -111,14 +111,14 @@ pt_status pt_attention_bwd(const pt_attention* a, const pt_heads* q, const pt_he
                            size_t ws_bytes, void* hip_stream) {
   size_t need = 0;
   pt_status s = pt_attention_workspace(a, &need);
-  if (s == PT_OK) s = check_view("q", q, a->nb, a->Sq, a->H, a->dtype, false);
-  if (s == PT_OK) s = check_view("k", k, a->nb, a->Sk, a->Hkv, a->dtype, false);
-  if (s == PT_OK) s = check_view("v", v, a->nb, a->Sk, a->Hkv, a->dtype, false);
-  if (s == PT_OK) s = check_view("o", o, a->nb, a->Sq, a->H, a->dtype, false);
-  if (s == PT_OK) s = check_view("d_o", d_o, a->nb, a->Sq, a->H, a->dtype, false);
-  if (s == PT_OK) s = check_view("dq", dq, a->nb, a->Sq, a->H, a->dtype, true);
-  if (s == PT_OK) s = check_view("dk", dk, a->nb, a->Sk, a->Hkv, a->dtype, true);
-  if (s == PT_OK) s = check_view("dv", dv, a->nb, a->Sk, a->Hkv, a->dtype, true);
+  if (s == PT_OK) s = check_view("q", q, a->nb, a->Sq, a->H, a, false);
+  if (s == PT_OK) s = check_view("k", k, a->nb, a->Sk, a->Hkv, a, false);
+  if (s == PT_OK) s = check_view("v", v, a->nb, a->Sk, a->Hkv, a, false);
+  if (s == PT_OK) s = check_view("o", o, a->nb, a->Sq, a->H, a, false);
+  if (s == PT_OK) s = check_view("d_o", d_o, a->nb, a->Sq, a->H, a, false);
+  if (s == PT_OK) s = check_view("dq", dq, a->nb, a->Sq, a->H, a, true);
+  if (s == PT_OK) s = check_view("dk", dk, a->nb, a->Sk, a->Hkv, a, true);
+  if (s == PT_OK) s = check_view("dv", dv, a->nb, a->Sk, a->Hkv, a, true);
   if (s != PT_OK) return s;
   if (a->nb == 0) return PT_OK;
   if (!lse && a->Sq > 0) return fail(PT_EINVAL, "lse is NULL");
