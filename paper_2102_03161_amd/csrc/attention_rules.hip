@@ -18,9 +18,9 @@
 // What bounds it: per pair and head the forward pass takes 4 dh flops of MFMA and about 2.5 VALU instructions (exp2 is a quarter
 // rate one), dq 8 dh (two products for the score and dP, two for dq and its correction), dk / dv 8 dh; at a head size of 64 the
 // VALU work takes about as long as the MFMAs, and of the four waves of a SIMD only some overlap the two: 740 - 830 TFLOP/s forward in
-// the steady state, 840 - 920 at 128 (a large product reaches 1444).  Measured: 32 x 384 rows x 12 heads of 64, padded, 39 us
-// forward, 59 dq, 61 dk / dv; 4 x 2048 x 16 packed, prefix, cap 61 / 107 / 89; 1 x 8192 x 16 of 128, causal, 4 key heads, forward
-// 317 (867 TFLOP/s of the visible pairs).  Tiles of 64 rows: two buffers of two take 32 KB at a head size of 64, so four workgroups
+// the steady state, 840 - 920 at 128 (a large product reaches 1444).  Measured (medians of a trace): 32 x 384 rows x 12 heads of 64,
+// padded, 37 us forward, 59 dq, 58 dk / dv; 4 x 2048 x 16 packed, prefix, cap 58 / 103 / 83; 1 x 8192 x 16 of 128, causal, 4 key heads,
+// forward 353, and 319 a call with pauses in between (860 TFLOP/s of the visible pairs).  Tiles of 64 rows: two buffers of two take 32 KB at a head size of 64, so four workgroups
 // fit a CU and hide each other's barriers, first loads and lists.
 #include "attention_rules.h"
 
@@ -163,8 +163,9 @@ struct Tile {
 };
 
 // 16 bytes a lane from global memory to LDS, lanes next to each other from `to` on, without a register in between.  Written as
-// assembly because the compiler, for the builtin, waits for such loads in front of every LDS read; all of them are waited for by
-// loads_done(), in front of the barrier behind which the tile is read.
+// assembly because the compiler, for the builtin, waits for such loads in front of every LDS read.  loads_done() waits for all of them, in
+// front of the barrier behind which the tile is read.  Where registers are spilled inside the loop (below), the compiler's wait for a
+// reload is one for the loads in front of it too, these among them.
 __device__ __forceinline__ void load_to_lds(unsigned to, const void* from) {
   unsigned kept;   // m0 as it was: the compiler may hold something in it
   asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
@@ -277,8 +278,9 @@ __device__ __forceinline__ void four(const int* p, int (&x)[4]) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
-// forward: one pass over the tiles with the running reference and sum of a softmax; four workgroups a CU at a head size of 64 (126
-// registers), two at 128.  At short rows it is bound by starting up: of 39 us for 32 x 384 x 12, padded, the visible pairs' products take 5.
+// forward: one pass over the tiles with the running reference and sum of a softmax; four workgroups a CU at a head size of 64 (128
+// registers, where a wave owns its rows alone 2 to 16 values more are spilled, none with a cap and without slopes), two at 128.  At short
+// rows it is bound by starting up: of 37 us for 32 x 384 x 12, padded, the visible pairs' products take 5.
 // ---------------------------------------------------------------------------------------------------------------------------
 // Two waves that share their rows: the second one's accumulators through LDS (both buffers' tiles, which nothing reads any more),
 // 16 bytes a lane next to each other.
@@ -463,8 +465,9 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
 // ---------------------------------------------------------------------------------------------------------------------------
 // backward: dq (128 queries a workgroup), which also leaves each query's delta, then dk and dv (128 keys a workgroup, the heads that
 // share them one after the other).  Two launches, because no workgroup sees all of a row and a column, and sums by atomics would
-// depend on their order.  Three workgroups a CU at a head size of 64 (168 registers); 272 - 312 registers at 128, one wave a SIMD,
-// which then waits for its own LDS reads: 12 x 384 rows x 10 heads of 128 take 108 us, of 64 49.
+// depend on their order.  Three workgroups a CU at a head size of 64 where a wave owns its rows alone (168 registers, and 9 to 21 values
+// spilled), two where two share them; 272 - 357 registers at 128, one wave a SIMD, which then waits for its own LDS reads: 12 x 384
+// rows x 10 heads of 128 take 108 us, of 64 49.
 // ---------------------------------------------------------------------------------------------------------------------------
 // delta_i = dO_i . o_i with o rounded to bf16 is off by 2^-9 of |dO||o|, which for a query with few keys, or one that takes most
 // of the weight, is as large as dS itself.  So the pass uses that value d only to centre dP, and takes out what is left of it:

@@ -52,8 +52,8 @@ __device__ __forceinline__ void decode4(uint32_t w, float step, float* x) {
   for (int i = 0; i < 4; ++i) x[i] = ((float)(w >> (8 * i) & 0xffu) - 128.f) * step;
 }
 
-// Phi, and phi.  bf16 results: the rational approximation of erfc of gelu_cdf() (4e-7), with the factors folded into its
-// coefficients; fp32 results: the library's erfc and exp.
+// Phi, and phi.  bf16 results: the rational approximation of erfc of gelu_cdf() (4e-7 absolute: 0.2 % of Phi at -5 and 1 % at -8, where x
+// Phi(x) is 1e-6 and 5e-15), with the factors folded into its coefficients; fp32 results: the library's erfc and exp.
 template <typename T> __device__ __forceinline__ float cdf_of(float x, float* pdf);
 template <> __device__ __forceinline__ float cdf_of<bf16>(float x, float* pdf) {
   const float t = __builtin_amdgcn_rcpf(fmaf(0.23164189f, fabsf(x), 1.0f));
