@@ -6,9 +6,9 @@
 //
 // What a query sees: keys up to lim_i (its own position, the end of the sample's prefix, or the last key) of its own document.
 //
-// One wave owns 32 rows (queries in the forward pass and for dq, keys for dk / dv), or, where that makes too few workgroups, half of
-// the streamed rows of 32 rows, joined at the end; a workgroup of four waves streams the other side through LDS in tiles of 64 rows.
-// Scores are computed with the owned row as the MFMA's column, so that softmax statistics are one value per lane and the
+// One wave owns 32 rows (queries in the forward pass and for dq, keys for dk / dv), or, where that makes too few workgroups
+// (attention_choice.h), half of the streamed rows of 32 rows, joined at the end; a workgroup of four waves streams the other side
+// through LDS in tiles of 64 rows.  Scores are computed with the owned row as the MFMA's column, so that softmax statistics are one value per lane and the
 // probabilities, rounded to bf16, are the next MFMA's operand as they stand in registers.
 //
 // Work that a mask leaves out is not done: before anything else a workgroup writes the list of the tiles that any of its waves
@@ -20,8 +20,8 @@
 // VALU work takes about as long as the MFMAs, and of the four waves of a SIMD only some overlap the two: 740 - 830 TFLOP/s forward in
 // the steady state, 840 - 920 at 128 (a large product reaches 1444).  Measured (medians of a trace): 32 x 384 rows x 12 heads of 64,
 // padded, 37 us forward, 59 dq, 58 dk / dv; 4 x 2048 x 16 packed, prefix, cap 58 / 103 / 83; 1 x 8192 x 16 of 128, causal, 4 key heads,
-// forward 353, and 319 a call with pauses in between (860 TFLOP/s of the visible pairs).  Tiles of 64 rows: two buffers of two take 32 KB at a head size of 64, so four workgroups
-// fit a CU and hide each other's barriers, first loads and lists.
+// forward 353, and 319 a call with pauses in between (860 TFLOP/s of the visible pairs).  Tiles of 64 rows: two buffers of two take 32 KB
+// at a head size of 64, so four workgroups fit a CU and hide each other's barriers, first loads and lists.
 #include "attention_rules.h"
 
 namespace pt {
@@ -465,7 +465,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
 // ---------------------------------------------------------------------------------------------------------------------------
 // backward: dq (128 queries a workgroup), which also leaves each query's delta, then dk and dv (128 keys a workgroup, the heads that
 // share them one after the other).  Two launches, because no workgroup sees all of a row and a column, and sums by atomics would
-// depend on their order.  Three workgroups a CU at a head size of 64 where a wave owns its rows alone (168 registers, and 9 to 21 values
+// depend on their order.  Three workgroups a CU at a head size of 64 where a wave owns its rows alone (168 registers, and 3 to 26 values
 // spilled), two where two share them; 272 - 357 registers at 128, one wave a SIMD, which then waits for its own LDS reads: 12 x 384
 // rows x 10 heads of 128 take 108 us, of 64 49.
 // ---------------------------------------------------------------------------------------------------------------------------
@@ -477,7 +477,10 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 : 2) void rule_fwd_kernel(AttnRul
 // roundings that all keys share, which dS itself, summing to 0, does not have, then cancels.
 // A query that sees one key has dS = 0, where dP - delta would leave the rounding of two different sums.  The pass counts the keys that
 // have some weight, in masked tiles (a whole one has several) and only until each of the wave's queries has met two, as lane masks in
-// scalar registers: the kernel has no vector register left.  The keys' pass finds a mark in place of such a query's delta.
+// scalar registers: the kernel has no vector register left.  The keys' pass finds a mark in place of such a query's delta, and looks
+// for it in masked tiles only: a query whose weights vanish beside one must not be marked where it sees 32 keys that one wave owns
+// there, so seeing the first and the last of those counts as two, whatever their weights.  (Counting by the masks throughout
+// makes the compiler keep them all: 193 us back against 155 at 4 x 2048 x 16.)
 constexpr uint32_t kOneKey = 0x7fc0a11eu;   // a NaN that no operation makes
 
 template <int DP, int MOD, int SHARE, bool FEW>
@@ -565,6 +568,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 4 - SHARE : 1) void rule_dq_kernel(
               two |= one & here;
               one |= here;
             }
+            const int* ends = kdoc + (it & 1) * kRuleTile + 32 * (x0 + st) + 4 * half;
+            two |= __ballot(ends[0] == qd && ends[27] == qd && (g.order == 0 || 32 * st + 27 <= far));
           }
         } else {
           two = ~0ull;

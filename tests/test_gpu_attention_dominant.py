@@ -9,6 +9,7 @@ import pytest
 import torch
 
 from paper_2102_03161_amd import binding
+from tests.test_gpu_attention_rules import compare
 
 pytestmark = pytest.mark.gpu
 BF16, F32 = torch.bfloat16, torch.float32
@@ -125,3 +126,16 @@ def test_one_visible_key_of_a_large_score(nb, S, H, dh, cap, dtype):
     got = gradients(q, k, v, do, docs, cap)
     assert torch.equal(got["o"], v)
     assert not got["dq"].any() and not got["dk"].any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("cap", [0.0, 900.0])
+@pytest.mark.parametrize("nb,S,H,order", [(1, 200, 2, "causal"), (13, 200, 20, "causal"), (1, 64, 2, "causal"), (2, 300, 2, "prefix"), (13, 200, 20, "prefix")])
+def test_weights_that_vanish_beside_one(nb, S, H, order, cap, dtype):
+    """Scores hundreds above all others: the other keys are visible, and their weights are 0 in fp32.  (The prefix ends inside a tile of
+    keys, so that a block of keys is whole for queries whose tiles are not.)"""
+    gen = torch.Generator().manual_seed(S)
+    k, v, do = (torch.randn(nb, S, H, 64, generator=gen).to(dtype) for _ in range(3))
+    at = (torch.rand(S, generator=gen) * torch.arange(1, S + 1)).long()      # a key that each query sees
+    q = (60.0 * k[:, at].float()).to(dtype)
+    compare(q.cuda(), k.cuda(), v.cuda(), do.cuda(), order=order, cap=cap, prefix=torch.full((nb,), 40, dtype=torch.int32) if order == "prefix" else None)
