@@ -19,8 +19,8 @@
 // rate one), dq 8 dh (two products for the score and dP, two for dq and its correction), dk / dv 8 dh; at a head size of 64 the
 // VALU work takes about as long as the MFMAs, and of the four waves of a SIMD only some overlap the two: 740 - 830 TFLOP/s forward in
 // the steady state, 840 - 920 at 128 (a large product reaches 1444).  Measured (medians of a trace): 32 x 384 rows x 12 heads of 64,
-// padded, 37 us forward, 59 dq, 58 dk / dv; 4 x 2048 x 16 packed, prefix, cap 58 / 103 / 83; 1 x 8192 x 16 of 128, causal, 4 key heads,
-// forward 353, and 319 a call with pauses in between (860 TFLOP/s of the visible pairs).  Tiles of 64 rows: two buffers of two take 32 KB
+// padded, 38 us forward, 59 dq, 60 dk / dv; 4 x 2048 x 16 packed, prefix, cap 57 / 103 / 83; 1 x 8192 x 16 of 128, causal, 4 key heads,
+// forward 357, and 321 a call with pauses in between (856 TFLOP/s of the visible pairs).  Tiles of 64 rows: two buffers of two take 32 KB
 // at a head size of 64, so four workgroups fit a CU and hide each other's barriers, first loads and lists.
 #include "attention_rules.h"
 
@@ -280,7 +280,7 @@ __device__ __forceinline__ void four(const int* p, int (&x)[4]) {
 // ---------------------------------------------------------------------------------------------------------------------------
 // forward: one pass over the tiles with the running reference and sum of a softmax; four workgroups a CU at a head size of 64 (128
 // registers, where a wave owns its rows alone 2 to 16 values more are spilled, none with a cap and without slopes), two at 128.  At short
-// rows it is bound by starting up: of 37 us for 32 x 384 x 12, padded, the visible pairs' products take 5.
+// rows it is bound by starting up: of 38 us for 32 x 384 x 12, padded, the visible pairs' products take 5.
 // ---------------------------------------------------------------------------------------------------------------------------
 // Two waves that share their rows: the second one's accumulators through LDS (both buffers' tiles, which nothing reads any more),
 // 16 bytes a lane next to each other.
